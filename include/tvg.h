@@ -1,5 +1,6 @@
 /*
- * libtvg - fused conv2d and depthwise conv2d operators for one AMD MI355X (gfx950).
+ * libtvg - fused conv2d and depthwise conv2d operators for one AMD MI355X (gfx950), and the
+ * channels-last operators that stand beside them: group norm, projections with adapters.
  *
  * These are hand-written versions of the fused tensor operators that the TVM
  * paper (arXiv 1802.04799) generates: a convolution with the element-wise
@@ -266,6 +267,74 @@ tvg_status tvg_dwpw_fused(const tvg_conv_desc *dw_desc, int32_t pw_k, uint32_t p
  */
 tvg_status tvg_maxpool2d_3x3s2(int32_t n, int32_t c, int32_t h, int32_t w, int32_t dtype,
                                const void *x, void *y, void *hip_stream);
+
+/*
+ * The last step of the channels-last operators below: none, max(t, 0) (a NaN stays one), t / (1 + exp(-t)).
+ */
+typedef enum { TVG_ACT_NONE = 0, TVG_ACT_RELU = 1, TVG_ACT_SILU = 2 } tvg_activation;
+
+/*
+ * Group norm with an activation over channels-last maps, forward and backward.
+ *   mean, var  over the pixels * (c / groups) elements of a group of a sample (var divides by their number)
+ *   rstd = 1 / sqrt(var + eps),  xhat = (x - mean) * rstd,  z = gamma[c] * xhat + beta[c],  y = act(z)
+ * x, y, dy, dx  device, [n][pixels][c], dtype (a map [n][h][w][c], a sequence [n][length][c]), dense
+ *   gamma, beta   device, fp32 [c], or NULL (ones, zeros)
+ *   mean, rstd    device, fp32 [n][groups]: written by the forward call, each may be NULL there; read by the backward call
+ *   dgamma, dbeta device, fp32 [c], written; each may be NULL
+ * Statistics and sums are fp32 (variances as sums of squared distances from a mean, so a large mean costs no digits);
+ * y and dx are rounded once.  dy' of ReLU at z <= 0 is 0.  y may be x; dx may be dy or x; otherwise outputs must not overlap
+ * inputs.
+ * flags must be 0.  Any alignment of whole elements (fp32 ones 4 bytes); 16 bytes and c a multiple of 8 (bf16) or 4 (fp32)
+ * are the fast way.
+ * Errors: TVG_ERR_BAD_SHAPE for extents below 1, c no multiple of groups, eps negative or not finite; TVG_ERR_UNSUPPORTED for
+ * unknown dtype, activation or flags, 2^31 elements, 2^30 pixels, n of 2^18
+ * or c of 2^20 or more; TVG_ERR_WORKSPACE for a
+ * workspace that is NULL, short or not 256-byte aligned (where the query says more than 0 bytes).
+ */
+typedef struct {
+    int32_t n, pixels, c, groups;
+    int32_t dtype;             /* tvg_dtype of x, y, dy, dx */
+    int32_t activation;        /* tvg_activation            */
+    float eps;
+    uint32_t flags;            /* 0                         */
+} tvg_group_norm_desc;
+tvg_status tvg_group_norm_workspace_size(const tvg_group_norm_desc *desc, size_t *bytes);
+tvg_status tvg_group_norm_fused(const tvg_group_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *y,
+                                float *mean, float *rstd, void *workspace, size_t workspace_bytes, void *hip_stream);
+tvg_status tvg_group_norm_backward_workspace_size(const tvg_group_norm_desc *desc, size_t *bytes);
+tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const void *x, const void *dy, const float *mean,
+                                         const float *rstd, const float *gamma, const float *beta, void *dx, float *dgamma,
+                                         float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Projection of rows (a 1x1 convolution of channels-last pixels, a linear layer of tokens) with a low-rank adapter chosen row
+ * by row, for batches that hold rows of many requests:
+ *   t = x W^T + bias + scale[i] * (x A_i^T) B_i^T + residual,  y = act(t),  i = adapter[row]
+ *   x        device, [rows][c], dtype          w   device, [k][c], dtype
+ *   a        device, [adapters][rank][c]       b   device, [adapters][k][rank], dtype (an adapter of a lower rank: zeros)
+ *   adapter  device, int32 [rows]; any value outside [0, adapters) is a row without an adapter
+ *   scale    device, fp32 [adapters], or NULL (ones)
+ *   bias     device, fp32 [k], or NULL         residual  device, [rows][k], dtype, or NULL
+ *   y        device, [rows][k], dtype, written completely; may be residual, else must not overlap an input
+ * All sums are fp32, the adapter's middle vector too: bf16 operands of the matrix cores hold it in two parts, 16 bits together.
+ * A row's result does not depend on the adapters of the other rows (what they hold, infinities and NaN included), and sums are
+ * added in a fixed order.
+ * rows == 0 is TVG_OK and launches nothing.  adapters == 0 is a plain projection: a, b, adapter and scale are ignored.
+ * flags must be 0.  Any alignment of whole elements; the fast way is 16-byte alignment of x, w, a and y, c and k multiples of 8
+ * (bf16) or 4 (fp32).
+ * Errors: TVG_ERR_BAD_SHAPE for c, k or rank below 1, rows or adapters below 0; TVG_ERR_UNSUPPORTED for unknown dtype,
+ * activation or flags, rank above 256, rows, c or k of 2^24 or more and tensors of 2^31 elements or more; TVG_ERR_WORKSPACE as above.
+ */
+typedef struct {
+    int32_t rows, c, k, adapters, rank;
+    int32_t dtype;             /* tvg_dtype of x, w, a, b, residual, y */
+    int32_t activation;        /* tvg_activation                       */
+    uint32_t flags;            /* 0                                    */
+} tvg_linear_lora_desc;
+tvg_status tvg_linear_lora_workspace_size(const tvg_linear_lora_desc *desc, size_t *bytes);
+tvg_status tvg_linear_lora_fused(const tvg_linear_lora_desc *desc, const void *x, const void *w, const void *a, const void *b,
+                                 const int32_t *adapter, const float *scale, const float *bias, const void *residual, void *y,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Static memory plan (TVM paper Section 3: after fusion a static memory planning pass

@@ -13,6 +13,8 @@ from .binding import (  # noqa: F401
     KERNEL_NAMES, tvg_conv2d_get_plan, tvg_conv2d_set_tile, ConvKnobs, tvg_conv2d_set_knobs, tvg_conv2d_get_knobs,
     tvg_static_scratch_bytes, tvg_conv2d_prepack_size, tvg_conv2d_prepack,
     tvg_probe_copy, tvg_probe_mfma, TVG_CENTRE_TAP_ONLY,
+    TVG_ACT_NONE, TVG_ACT_RELU, TVG_ACT_SILU, GroupNormDesc, LinearLoraDesc, tvg_group_norm_workspace_size,
+    tvg_group_norm_backward_workspace_size, tvg_linear_lora_workspace_size,
     TensorLife, tvg_plan_arena, tvg_dwpw_one_kernel, tvg_dwpw_workspace_size,
 )
 

@@ -19,6 +19,7 @@ TVG_F32, TVG_BF16 = 0, 1
 TVG_RELU = 1
 TVG_STREAM_OUT = 2      # hint: nothing reads y soon, store it past the caches
 TVG_CENTRE_TAP_ONLY = 4  # flags2 of tvg_conv2d_fused_dual: head 2's filters are zero off the centre tap
+TVG_ACT_NONE, TVG_ACT_RELU, TVG_ACT_SILU = 0, 1, 2      # tvg_activation
 TVG_OK = 0
 
 
@@ -43,6 +44,18 @@ class ConvDesc(ctypes.Structure):
     @property
     def ow(self) -> int:
         return (self.w + 2 * self.pad_w - self.s) // self.stride_w + 1
+
+
+class GroupNormDesc(ctypes.Structure):
+    """Mirror of tvg_group_norm_desc."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n", "pixels", "c", "groups", "dtype", "activation")] + \
+               [("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class LinearLoraDesc(ctypes.Structure):
+    """Mirror of tvg_linear_lora_desc."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "c", "k", "adapters", "rank", "dtype", "activation")] + \
+               [("flags", ctypes.c_uint32)]
 
 
 class ConvKnobs(ctypes.Structure):
@@ -132,6 +145,15 @@ def load() -> ctypes.CDLL:
     i32p = ctypes.POINTER(ctypes.c_int32)
     lib.tvg_conv2d_get_plan.restype = ctypes.c_int
     lib.tvg_conv2d_get_plan.argtypes = [dp, i32p, i32p, i32p]
+    np, lp = ctypes.POINTER(GroupNormDesc), ctypes.POINTER(LinearLoraDesc)
+    for f, kind in ((lib.tvg_group_norm_workspace_size, np), (lib.tvg_group_norm_backward_workspace_size, np),
+                    (lib.tvg_linear_lora_workspace_size, lp)):
+        f.restype = ctypes.c_int
+        f.argtypes = [kind, ctypes.POINTER(sz)]
+    for f, kind, addresses in ((lib.tvg_group_norm_fused, np, 7), (lib.tvg_group_norm_fused_backward, np, 10),
+                               (lib.tvg_linear_lora_fused, lp, 10)):
+        f.restype = ctypes.c_int
+        f.argtypes = [kind] + [vp] * addresses + [sz, vp]
     _lib = lib
     return lib
 
@@ -150,8 +172,14 @@ _RAW = {
     "tvg_dwpw_fused": ("dw_desc pw_k pw_flags x w_dw scale_dw shift_dw w_pw scale_pw shift_pw bias_pw residual y "
                        "workspace workspace_bytes stream", "diipppppppppppus", 3),
     "tvg_maxpool2d_3x3s2": ("n c h w dtype x y stream", "uuuuupps", 1),
+    "tvg_group_norm_fused": ("desc x gamma beta y mean rstd workspace workspace_bytes stream", "dpppppppus", 3),
+    "tvg_group_norm_fused_backward": ("desc x dy mean rstd gamma beta dx dgamma dbeta workspace workspace_bytes stream",
+                                      "dppppppppppus", 3),
+    "tvg_linear_lora_fused": ("desc x w a b adapter scale bias residual y workspace workspace_bytes stream",
+                              "dppppppppppus", 3),
 }
-NATIVE_NAMES = tuple(_RAW) + ("conv2d_fused", "dwconv2d_fused", "dwpw_fused")
+NATIVE_NAMES = tuple(_RAW) + ("conv2d_fused", "dwconv2d_fused", "dwpw_fused", "group_norm_fused",
+                              "group_norm_fused_backward", "linear_lora_fused")
 _native = None
 
 
@@ -163,7 +191,7 @@ def native():
         import torch  # noqa: F401  (the extension links against the libraries torch has loaded)
         from importlib import import_module
         module = import_module("._native", __package__)
-        module.setup(ConvDesc, TvgError, _CONVENIENCES)
+        module.setup(ConvDesc, TvgError, _CONVENIENCES, GroupNormDesc, LinearLoraDesc)
         _native = module
     return _native
 
@@ -321,6 +349,26 @@ def tvg_dwpw_workspace_size(dw_desc: ConvDesc, pw_k: int) -> int:
     if st != TVG_OK:
         raise TvgError(st, "tvg_dwpw_workspace_size")
     return int(out.value)
+
+
+def _workspace_size(name, desc) -> int:
+    out = ctypes.c_size_t(0)
+    st = getattr(load(), name)(ctypes.byref(desc), ctypes.byref(out))
+    if st != TVG_OK:
+        raise TvgError(st, name)
+    return int(out.value)
+
+
+def tvg_group_norm_workspace_size(desc: GroupNormDesc) -> int:
+    return _workspace_size("tvg_group_norm_workspace_size", desc)
+
+
+def tvg_group_norm_backward_workspace_size(desc: GroupNormDesc) -> int:
+    return _workspace_size("tvg_group_norm_backward_workspace_size", desc)
+
+
+def tvg_linear_lora_workspace_size(desc: LinearLoraDesc) -> int:
+    return _workspace_size("tvg_linear_lora_workspace_size", desc)
 
 
 def tvg_dwpw_one_kernel(dw_desc: ConvDesc, pw_k: int) -> bool:
@@ -497,5 +545,152 @@ def maxpool2d_3x3s2(x, out=None, stream=None):
     return out
 
 
-_CONVENIENCES = {"conv2d_fused": _conv2d_fused, "dwconv2d_fused": _dwconv2d_fused, "dwpw_fused": _dwpw_fused}
+# ---------------------------------------------------------------------------------------
+# channels-last operators
+# ---------------------------------------------------------------------------------------
+
+_ACTIVATIONS = {None: TVG_ACT_NONE, "relu": TVG_ACT_RELU, "silu": TVG_ACT_SILU}
+
+
+def _activation(name) -> int:
+    if name not in _ACTIVATIONS:
+        raise ValueError(f"activation must be None, 'relu' or 'silu', not {name!r}")
+    return _ACTIVATIONS[name]
+
+
+def _operand(x, name, t, dtype, count=None, shape=None, optional=False):
+    """Refuses an operand that is not a dense tensor of this type and size on x's device."""
+    if t is None:
+        if optional:
+            return
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.device != x.device:
+        raise ValueError(f"{name} is on {t.device}, x on {x.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{name} must have {count} elements, not {t.numel()}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _buffer_beside(x, name, t):
+    if t is not None and getattr(t, "device", x.device) != x.device:
+        raise ValueError(f"{name} is on {t.device}, x on {x.device}")
+
+
+def _on_device(x):
+    """Launches go to the current device: x's, for the time of a call."""
+    import contextlib
+    import torch
+    return torch.cuda.device(x.device) if torch.cuda.is_initialized() else contextlib.nullcontext()
+
+
+def _norm_desc(x, groups, eps, activation) -> GroupNormDesc:
+    _operand(x, "x", x, x.dtype)
+    if x.dim() < 2:
+        raise ValueError("x must be [n][...][c]")
+    n, c = x.shape[0], x.shape[-1]
+    pixels = math.prod(x.shape[1:-1])
+    if max(n, c, pixels) >= 1 << 31:
+        raise ValueError("x is too large")
+    return GroupNormDesc(n, pixels, c, int(groups), _dtype_code(x), _activation(activation), float(eps), 0)
+
+
+def _group_norm_fused(x, groups, gamma=None, beta=None, *, eps=1e-5, activation=None, stats=False, out=None, workspace=None,
+                      stream=None):
+    """y = act(group norm of x [n][...][c]), or (y, mean, rstd) with ``stats``; allocates what is not given with torch."""
+    import torch
+    desc = _norm_desc(x, groups, eps, activation)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _operand(x, name, t, torch.float32, desc.c, optional=True)
+    need = tvg_group_norm_workspace_size(desc)
+    _buffer_beside(x, "out", out)
+    _buffer_beside(x, "workspace", workspace)
+    with _on_device(x):
+        y = _output(out, lambda: tuple(x.shape), x, stream)
+        mean, rstd = (_empty((desc.n, desc.groups), torch.float32, x.device, stream) if stats else None for _ in range(2))
+        if need:
+            workspace = _workspace(workspace, need, x, stream)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = native().tvg_group_norm_fused(desc, x, gamma, beta, y, mean, rstd, workspace, ws_bytes, stream)
+    if st != TVG_OK:
+        raise TvgError(st, "tvg_group_norm_fused")
+    return (y, mean, rstd) if stats else y
+
+
+def _group_norm_fused_backward(x, dy, mean, rstd, groups, gamma=None, beta=None, *, activation=None, out=None, workspace=None,
+                               stream=None):
+    """(dx, dgamma, dbeta) of group_norm_fused; dgamma and dbeta are None where gamma and beta are."""
+    import torch
+    desc = _norm_desc(x, groups, 0.0, activation)
+    _operand(x, "dy", dy, x.dtype, shape=x.shape)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _operand(x, name, t, torch.float32, desc.n * desc.groups)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _operand(x, name, t, torch.float32, desc.c, optional=True)
+    need = tvg_group_norm_backward_workspace_size(desc)
+    _buffer_beside(x, "out", out)
+    _buffer_beside(x, "workspace", workspace)
+    with _on_device(x):
+        dx = _output(out, lambda: tuple(x.shape), x, stream)
+        dgamma, dbeta = (None if t is None else _empty((desc.c,), torch.float32, x.device, stream) for t in (gamma, beta))
+        if need:
+            workspace = _workspace(workspace, need, x, stream)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = native().tvg_group_norm_fused_backward(desc, x, dy, mean, rstd, gamma, beta, dx, dgamma, dbeta, workspace, ws_bytes,
+                                                    stream)
+    if st != TVG_OK:
+        raise TvgError(st, "tvg_group_norm_fused_backward")
+    return dx, dgamma, dbeta
+
+
+def _linear_lora_fused(x, w, a, b, adapter, scale=None, bias=None, residual=None, *, activation=None, out=None, workspace=None,
+                       stream=None):
+    """y = act(x w^T + bias + scale_i (x a_i^T) b_i^T + residual) of rows x [...][c], i = adapter of the row; a, b and
+    adapter may be None together (a plain projection)."""
+    import torch
+    _operand(x, "x", x, x.dtype)
+    if x.dim() < 1:
+        raise ValueError("x must be [...][c]")
+    c = x.shape[-1]
+    if w is None or w.dim() != 2:
+        raise ValueError("w must be [k][c]")
+    k, rows = w.shape[0], math.prod(x.shape[:-1])
+    _operand(x, "w", w, x.dtype, shape=(k, c))
+    n, r = 0, 1
+    if a is not None or b is not None or adapter is not None:
+        if a is None or a.dim() != 3:
+            raise ValueError("a must be [adapters][rank][c]")
+        n, r = a.shape[0], a.shape[1]
+        _operand(x, "a", a, x.dtype, shape=(n, r, c))
+        _operand(x, "b", b, x.dtype, shape=(n, k, r))
+        _operand(x, "adapter", adapter, torch.int32, rows)
+        _operand(x, "scale", scale, torch.float32, n, optional=True)
+    _operand(x, "bias", bias, torch.float32, k, optional=True)
+    _operand(x, "residual", residual, x.dtype, rows * k, optional=True)
+    if max(rows, c, k, n, r) >= 1 << 31:
+        raise ValueError("an operand is too large")
+    desc = LinearLoraDesc(rows, c, k, n, r, _dtype_code(x), _activation(activation), 0)
+    need = tvg_linear_lora_workspace_size(desc)
+    _buffer_beside(x, "out", out)
+    _buffer_beside(x, "workspace", workspace)
+    with _on_device(x):
+        y = _output(out, lambda: tuple(x.shape[:-1]) + (k,), x, stream)
+        if need:
+            workspace = _workspace(workspace, need, x, stream)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = native().tvg_linear_lora_fused(desc, x, w, a, b, adapter, scale, bias, residual, y, workspace, ws_bytes, stream)
+    if st != TVG_OK:
+        raise TvgError(st, "tvg_linear_lora_fused")
+    return y
+
+
+_CONVENIENCES = {"conv2d_fused": _conv2d_fused, "dwconv2d_fused": _dwconv2d_fused, "dwpw_fused": _dwpw_fused,
+                 "group_norm_fused": _group_norm_fused, "group_norm_fused_backward": _group_norm_fused_backward,
+                 "linear_lora_fused": _linear_lora_fused}
 __all__ = [_n for _n in globals() if not _n.startswith("_")] + list(NATIVE_NAMES)

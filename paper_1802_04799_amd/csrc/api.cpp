@@ -1,5 +1,6 @@
 // C ABI of libtvg: argument validation (host only, before any device call),
 // planning and dispatch to the kernel launchers.
+#include <float.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -739,6 +740,122 @@ tvg_status tvg_maxpool2d_3x3s2(int32_t n, int32_t c, int32_t h, int32_t w, int32
     if (count_elems({n, c, h, w}) >= kMaxElems) return TVG_ERR_UNSUPPORTED;
     if (!x || !y) return TVG_ERR_NULL;
     return tvg::launch_maxpool3x3s2(n, c, h, w, dtype, x, y, static_cast<hipStream_t>(hip_stream));
+}
+
+static bool known_types(int32_t dtype, int32_t activation, uint32_t flags)
+{
+    return (dtype == TVG_F32 || dtype == TVG_BF16) && activation >= TVG_ACT_NONE && activation <= TVG_ACT_SILU && flags == 0;
+}
+
+static bool workspace_ok(const void *workspace, size_t bytes, size_t need)
+{
+    return need == 0 || (workspace && bytes >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0);
+}
+
+static bool aligned_to(size_t bytes, std::initializer_list<const void *> pointers)
+{
+    for (const void *q : pointers)
+        if (reinterpret_cast<uintptr_t>(q) % bytes != 0) return false;
+    return true;
+}
+
+static tvg_status make_norm(const tvg_group_norm_desc *d, tvg::NormProblem *p)
+{
+    if (!d) return TVG_ERR_NULL;
+    if (d->n < 1 || d->pixels < 1 || d->c < 1 || d->groups < 1 || d->c % d->groups != 0) return TVG_ERR_BAD_SHAPE;
+    if (!(d->eps >= 0.0f && d->eps <= FLT_MAX)) return TVG_ERR_BAD_SHAPE;
+    if (!known_types(d->dtype, d->activation, d->flags)) return TVG_ERR_UNSUPPORTED;
+    if (count_elems({d->n, d->pixels, d->c}) >= kMaxElems || d->pixels >= 1 << 30 || d->n >= 1 << 18 || d->c >= 1 << 20)
+        return TVG_ERR_UNSUPPORTED;
+    *p = tvg::NormProblem{d->n, d->pixels, d->c, d->groups, d->activation, d->dtype, d->eps};
+    return TVG_OK;
+}
+
+static tvg_status norm_workspace(const tvg_group_norm_desc *desc, bool backward, size_t *bytes)
+{
+    if (!bytes) return TVG_ERR_NULL;
+    tvg::NormProblem p;
+    const tvg_status st = make_norm(desc, &p);
+    if (st == TVG_OK) *bytes = tvg::group_norm_workspace(p, backward);
+    return st;
+}
+
+tvg_status tvg_group_norm_workspace_size(const tvg_group_norm_desc *desc, size_t *bytes)
+{
+    return norm_workspace(desc, false, bytes);
+}
+
+tvg_status tvg_group_norm_backward_workspace_size(const tvg_group_norm_desc *desc, size_t *bytes)
+{
+    return norm_workspace(desc, true, bytes);
+}
+
+tvg_status tvg_group_norm_fused(const tvg_group_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *y,
+                                float *mean, float *rstd, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    tvg::NormProblem p;
+    const tvg_status st = make_norm(desc, &p);
+    if (st != TVG_OK) return st;
+    if (!x || !y) return TVG_ERR_NULL;
+    if (!aligned_to(p.dtype == TVG_BF16 ? 2 : 4, {x, y}) || !aligned_to(4, {gamma, beta, mean, rstd})) return TVG_ERR_UNSUPPORTED;
+    if (!workspace_ok(workspace, workspace_bytes, tvg::group_norm_workspace(p, false))) return TVG_ERR_WORKSPACE;
+    return tvg::launch_group_norm(p, x, gamma, beta, y, mean, rstd, static_cast<float *>(workspace),
+                                  static_cast<hipStream_t>(hip_stream));
+}
+
+tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const void *x, const void *dy, const float *mean,
+                                         const float *rstd, const float *gamma, const float *beta, void *dx, float *dgamma,
+                                         float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    tvg::NormProblem p;
+    const tvg_status st = make_norm(desc, &p);
+    if (st != TVG_OK) return st;
+    if (!x || !dy || !mean || !rstd || !dx) return TVG_ERR_NULL;
+    if (!aligned_to(p.dtype == TVG_BF16 ? 2 : 4, {x, dy, dx}) || !aligned_to(4, {mean, rstd, gamma, beta, dgamma, dbeta}))
+        return TVG_ERR_UNSUPPORTED;
+    if (!workspace_ok(workspace, workspace_bytes, tvg::group_norm_workspace(p, true))) return TVG_ERR_WORKSPACE;
+    return tvg::launch_group_norm_backward(p, x, dy, mean, rstd, gamma, beta, dx, dgamma, dbeta, static_cast<float *>(workspace),
+                                           static_cast<hipStream_t>(hip_stream));
+}
+
+static tvg_status make_lora(const tvg_linear_lora_desc *d, tvg::LoraProblem *p)
+{
+    if (!d) return TVG_ERR_NULL;
+    if (d->rows < 0 || d->c < 1 || d->k < 1 || d->adapters < 0 || d->rank < 1) return TVG_ERR_BAD_SHAPE;
+    if (!known_types(d->dtype, d->activation, d->flags) || d->rank > 256) return TVG_ERR_UNSUPPORTED;
+    if (d->rows >= 1 << 24 || d->c >= 1 << 24 || d->k >= 1 << 24) return TVG_ERR_UNSUPPORTED;
+    for (const int64_t n : {count_elems({std::max(d->rows, 1), d->c}), count_elems({std::max(d->rows, 1), d->k}),
+                            count_elems({d->k, d->c}), count_elems({std::max(d->adapters, 1), d->rank, d->c}),
+                            count_elems({std::max(d->adapters, 1), d->k, d->rank})})
+        if (n >= kMaxElems) return TVG_ERR_UNSUPPORTED;
+    *p = tvg::LoraProblem{d->rows, d->c, d->k, d->adapters, d->rank, d->activation, d->dtype};
+    return TVG_OK;
+}
+
+tvg_status tvg_linear_lora_workspace_size(const tvg_linear_lora_desc *desc, size_t *bytes)
+{
+    if (!bytes) return TVG_ERR_NULL;
+    tvg::LoraProblem p;
+    const tvg_status st = make_lora(desc, &p);
+    if (st == TVG_OK) *bytes = tvg::linear_lora_workspace(p);
+    return st;
+}
+
+tvg_status tvg_linear_lora_fused(const tvg_linear_lora_desc *desc, const void *x, const void *w, const void *a, const void *b,
+                                 const int32_t *adapter, const float *scale, const float *bias, const void *residual, void *y,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    tvg::LoraProblem p;
+    const tvg_status st = make_lora(desc, &p);
+    if (st != TVG_OK) return st;
+    if (p.rows == 0) return TVG_OK;
+    if (!x || !w || !y || (p.adapters > 0 && (!a || !b || !adapter))) return TVG_ERR_NULL;
+    if (p.adapters == 0) a = b = nullptr, adapter = nullptr, scale = nullptr;
+    if (!aligned_to(p.dtype == TVG_BF16 ? 2 : 4, {x, w, a, b, residual, y}) || !aligned_to(4, {adapter, scale, bias}))
+        return TVG_ERR_UNSUPPORTED;
+    if (!workspace_ok(workspace, workspace_bytes, tvg::linear_lora_workspace(p))) return TVG_ERR_WORKSPACE;
+    const tvg::LoraPointers ptr{x, w, a, b, adapter, scale, bias, residual, y, static_cast<float *>(workspace)};
+    return tvg::launch_linear_lora(p, ptr, static_cast<hipStream_t>(hip_stream));
 }
 
 const char *tvg_status_string(tvg_status status)

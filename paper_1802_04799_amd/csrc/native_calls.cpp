@@ -17,6 +17,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -29,6 +30,8 @@
 namespace {
 
 PyObject *g_desc_type = nullptr;       // binding.ConvDesc
+PyObject *g_norm_type = nullptr;       // binding.GroupNormDesc
+PyObject *g_lora_type = nullptr;       // binding.LinearLoraDesc
 PyObject *g_error_type = nullptr;      // binding.TvgError
 PyObject *g_fallback = nullptr;        // name -> Python implementation of a convenience call
 
@@ -142,22 +145,26 @@ bool as_integer(PyObject *o, long long fallback, long long *out)
     return ok;
 }
 
-bool descriptor(PyObject *o, tvg_conv_desc *out)
+template <typename D> bool descriptor_of(PyObject *type, const char *name, PyObject *o, D *out)
 {
-    const int is = PyObject_IsInstance(o, g_desc_type);
+    const int is = PyObject_IsInstance(o, type);
     if (is < 0) return false;
     Py_buffer view;
     if (!is) {
-        PyErr_Format(PyExc_TypeError, "desc must be a ConvDesc, not %s", Py_TYPE(o)->tp_name);
+        PyErr_Format(PyExc_TypeError, "desc must be a %s, not %s", name, Py_TYPE(o)->tp_name);
         return false;
     }
     if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) return false;
     const bool fits = view.len == (Py_ssize_t)sizeof(*out);
-    if (fits) *out = *static_cast<const tvg_conv_desc *>(view.buf);
+    if (fits) *out = *static_cast<const D *>(view.buf);
     PyBuffer_Release(&view);
     if (!fits) PyErr_SetString(PyExc_TypeError, "desc has the wrong size");
     return fits;
 }
+
+bool descriptor(PyObject *o, tvg_conv_desc *out) { return descriptor_of(g_desc_type, "ConvDesc", o, out); }
+bool descriptor(PyObject *o, tvg_group_norm_desc *out) { return descriptor_of(g_norm_type, "GroupNormDesc", o, out); }
+bool descriptor(PyObject *o, tvg_linear_lora_desc *out) { return descriptor_of(g_lora_type, "LinearLoraDesc", o, out); }
 
 // Runs a library call without the GIL, which is held again on every way out.  Nothing of torch's
 // belongs in `f`: reading a tensor's address may raise (tensors without storage), so callers read
@@ -226,6 +233,12 @@ SPEC(tvg_conv2d_fused_prepacked, 11, 10, "desc", "x", "packed", "scale", "shift"
 SPEC(tvg_dwpw_fused, 16, 13, "dw_desc", "pw_k", "pw_flags", "x", "w_dw", "scale_dw", "shift_dw", "w_pw", "scale_pw",
      "shift_pw", "bias_pw", "residual", "y", "workspace", "workspace_bytes", "stream");
 SPEC(tvg_maxpool2d_3x3s2, 8, 7, "n", "c", "h", "w", "dtype", "x", "y", "stream");
+
+SPEC(tvg_group_norm_fused, 10, 7, "desc", "x", "gamma", "beta", "y", "mean", "rstd", "workspace", "workspace_bytes", "stream");
+SPEC(tvg_group_norm_fused_backward, 13, 10, "desc", "x", "dy", "mean", "rstd", "gamma", "beta", "dx", "dgamma", "dbeta",
+     "workspace", "workspace_bytes", "stream");
+SPEC(tvg_linear_lora_fused, 13, 10, "desc", "x", "w", "a", "b", "adapter", "scale", "bias", "residual", "y", "workspace",
+     "workspace_bytes", "stream");
 
 #define ARGS PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames
 
@@ -341,6 +354,53 @@ PyObject *py_tvg_maxpool2d_3x3s2(ARGS)
         });
         return PyLong_FromLong(st);
     });
+}
+
+// A descriptor, N addresses, the workspace's bytes and the stream.
+template <typename D, int N, typename F>
+PyObject *addresses_call(const Spec &spec, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames, F &&f)
+{
+    return guarded([&]() -> PyObject * {
+        PyObject *v[N + 3];
+        D d;
+        void *p[N], *stream;
+        long long bytes;
+        if (!parse(spec, args, nargs, kwnames, v) || !descriptor(v[0], &d)) return nullptr;
+        for (int i = 0; i < N; ++i)
+            if (!address(v[1 + i], &p[i])) return nullptr;
+        if (!integer(v[N + 1], 0, &bytes) || !stream_handle(v[N + 2], &stream)) return nullptr;
+        return PyLong_FromLong(without_gil([&] { return f(&d, p, (size_t)bytes, stream); }));
+    });
+}
+
+PyObject *py_tvg_group_norm_fused(ARGS)
+{
+    return addresses_call<tvg_group_norm_desc, 7>(
+        tvg_group_norm_fused_spec, args, nargs, kwnames, [](const tvg_group_norm_desc *d, void **p, size_t bytes, void *stream) {
+            return tvg_group_norm_fused(d, p[0], static_cast<float *>(p[1]), static_cast<float *>(p[2]), p[3],
+                                        static_cast<float *>(p[4]), static_cast<float *>(p[5]), p[6], bytes, stream);
+        });
+}
+
+PyObject *py_tvg_group_norm_fused_backward(ARGS)
+{
+    return addresses_call<tvg_group_norm_desc, 10>(
+        tvg_group_norm_fused_backward_spec, args, nargs, kwnames,
+        [](const tvg_group_norm_desc *d, void **p, size_t bytes, void *stream) {
+            return tvg_group_norm_fused_backward(d, p[0], p[1], static_cast<float *>(p[2]), static_cast<float *>(p[3]),
+                                                 static_cast<float *>(p[4]), static_cast<float *>(p[5]), p[6],
+                                                 static_cast<float *>(p[7]), static_cast<float *>(p[8]), p[9], bytes, stream);
+        });
+}
+
+PyObject *py_tvg_linear_lora_fused(ARGS)
+{
+    return addresses_call<tvg_linear_lora_desc, 10>(
+        tvg_linear_lora_fused_spec, args, nargs, kwnames,
+        [](const tvg_linear_lora_desc *d, void **p, size_t bytes, void *stream) {
+            return tvg_linear_lora_fused(d, p[0], p[1], p[2], p[3], static_cast<int32_t *>(p[4]), static_cast<float *>(p[5]),
+                                         static_cast<float *>(p[6]), p[7], p[8], p[9], bytes, stream);
+        });
 }
 
 // ---------------------------------------------------------------------------------------
@@ -618,11 +678,219 @@ PyObject *py_dwpw_fused(ARGS)
     });
 }
 
-// setup(ConvDesc, TvgError, {name: Python implementation})
+// ---------------------------------------------------------------------------------------
+// channels-last operators
+// ---------------------------------------------------------------------------------------
+
+SPEC(group_norm_fused, 4, 2, "x", "groups", "gamma", "beta", "eps", "activation", "stats", "out", "workspace", "stream");
+SPEC(group_norm_fused_backward, 7, 5, "x", "dy", "mean", "rstd", "groups", "gamma", "beta", "activation", "out", "workspace",
+     "stream");
+SPEC(linear_lora_fused, 8, 5, "x", "w", "a", "b", "adapter", "scale", "bias", "residual", "activation", "out", "workspace",
+     "stream");
+
+// None, "relu" or "silu"
+bool activation_code(PyObject *o, int32_t *out)
+{
+    *out = TVG_ACT_NONE;
+    if (absent(o)) return true;
+    if (!PyUnicode_CheckExact(o)) return false;
+    if (PyUnicode_CompareWithASCIIString(o, "relu") == 0) *out = TVG_ACT_RELU;
+    else if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) *out = TVG_ACT_SILU;
+    else return false;
+    return true;
+}
+
+// Whether optional tensors lie on x's device and have `count` elements.
+bool beside(const at::Tensor &x, int64_t count, std::initializer_list<const at::Tensor *> tensors)
+{
+    for (const at::Tensor *t : tensors)
+        if (t && (t->numel() != count || t->device() != x.device())) return false;
+    return true;
+}
+
+// Whether an output or workspace of the caller's can be used for `bytes` bytes (a workspace that is too small is not used).
+bool holds(const at::Tensor *out, const at::Tensor &x, size_t bytes)
+{
+    return !out || (dense_on_device(*out) && out->device() == x.device() && bytes_of(out) >= bytes);
+}
+bool usable_beside(const at::Tensor *ws, const at::Tensor &x, size_t need)
+{
+    return bytes_of(ws) < need || !need || (dense_on_device(*ws) && ws->device() == x.device());
+}
+
+// x [n][...][c]
+bool describe_norm(const at::Tensor &x, PyObject *groups, float eps, int32_t activation, tvg_group_norm_desc *d)
+{
+    if (x.dim() < 2 || !extent(groups, &d->groups) || !known_dtype(x, &d->dtype)) return false;
+    const int64_t n = x.size(0), c = x.size(-1), total = x.numel();
+    if (n < 1 || c < 1 || total < 1 || total > INT32_MAX) return false;
+    d->n = (int32_t)n;
+    d->c = (int32_t)c;
+    d->pixels = (int32_t)(total / (n * c));
+    d->activation = activation;
+    d->eps = eps;
+    d->flags = 0;
+    return true;
+}
+
+PyObject *py_group_norm_fused(ARGS)
+{
+    return guarded([&]() -> PyObject * {
+        PyObject *v[10];
+        if (!parse(group_norm_fused_spec, args, nargs, kwnames, v)) return nullptr;
+        const auto other = [&] { return fall_back("group_norm_fused", args, nargs, kwnames); };
+        if (!THPVariable_CheckExact(v[0])) return other();
+        const at::Tensor *x, *gamma, *beta, *out, *ws;
+        bool stats;
+        int32_t act;
+        tvg_group_norm_desc d;
+        if (v[4] && !PyFloat_CheckExact(v[4])) return other();
+        const double eps = v[4] ? PyFloat_AS_DOUBLE(v[4]) : 1e-5;
+        if (!plain_tensor(v[0], false, THPVariable_Unpack(v[0]).scalar_type(), &x) || !plain_tensor(v[2], true, at::kFloat, &gamma) ||
+            !plain_tensor(v[3], true, at::kFloat, &beta) || !activation_code(v[5], &act) || !flag(v[6], false, &stats) ||
+            !plain_buffer(v[7], &out) || !plain_buffer(v[8], &ws) || !describe_norm(*x, v[1], (float)eps, act, &d) ||
+            !beside(*x, d.c, {gamma, beta}) || !holds(out, *x, bytes_of(x)))
+            return other();
+        size_t need = 0;
+        if (tvg_group_norm_workspace_size(&d, &need) != TVG_OK || !usable_beside(ws, *x, need)) return other();
+        const c10::DeviceGuard on(x->device());
+        void *stream;
+        if (!stream_handle(v[9], &stream)) return nullptr;
+        const Allocator memory(*x, v[9], stream);
+        at::Tensor y = out ? *out : memory.result(x->sizes(), x->scalar_type());
+        at::Tensor mean, rstd, scratch;
+        if (stats) {
+            mean = memory.result({d.n, d.groups}, at::kFloat);
+            rstd = memory.result({d.n, d.groups}, at::kFloat);
+        }
+        if (need) scratch = enough_workspace(ws, need, memory);
+        void *yp = y.data_ptr(), *sp = need ? scratch.data_ptr() : nullptr;
+        const void *xp = data(x);
+        const float *gp = floats(gamma), *bp = floats(beta);
+        float *mp = stats ? mean.data_ptr<float>() : nullptr, *rp = stats ? rstd.data_ptr<float>() : nullptr;
+        const size_t bytes = need ? bytes_of(&scratch) : 0;
+        const tvg_status st = without_gil([&] { return tvg_group_norm_fused(&d, xp, gp, bp, yp, mp, rp, sp, bytes, stream); });
+        if (st != TVG_OK) return raise_status(st, "tvg_group_norm_fused");
+        PyObject *result = out ? (Py_INCREF(v[7]), v[7]) : THPVariable_Wrap(std::move(y));
+        if (!stats || !result) return result;
+        return Py_BuildValue("(NNN)", result, THPVariable_Wrap(std::move(mean)), THPVariable_Wrap(std::move(rstd)));
+    });
+}
+
+PyObject *py_group_norm_fused_backward(ARGS)
+{
+    return guarded([&]() -> PyObject * {
+        PyObject *v[11];
+        if (!parse(group_norm_fused_backward_spec, args, nargs, kwnames, v)) return nullptr;
+        const auto other = [&] { return fall_back("group_norm_fused_backward", args, nargs, kwnames); };
+        if (!THPVariable_CheckExact(v[0])) return other();
+        const at::Tensor *x, *dy, *mean, *rstd, *gamma, *beta, *out, *ws;
+        int32_t act;
+        tvg_group_norm_desc d;
+        const c10::ScalarType dtype = THPVariable_Unpack(v[0]).scalar_type();
+        if (!plain_tensor(v[0], false, dtype, &x) || !plain_tensor(v[1], false, dtype, &dy) ||
+            !plain_tensor(v[2], false, at::kFloat, &mean) || !plain_tensor(v[3], false, at::kFloat, &rstd) ||
+            !plain_tensor(v[5], true, at::kFloat, &gamma) || !plain_tensor(v[6], true, at::kFloat, &beta) ||
+            !activation_code(v[7], &act) || !plain_buffer(v[8], &out) || !plain_buffer(v[9], &ws) ||
+            !describe_norm(*x, v[4], 0.0f, act, &d) || !beside(*x, d.c, {gamma, beta}) ||
+            !beside(*x, (int64_t)d.n * d.groups, {mean, rstd}) || dy->sizes() != x->sizes() || dy->device() != x->device() ||
+            !holds(out, *x, bytes_of(x)))
+            return other();
+        size_t need = 0;
+        if (tvg_group_norm_backward_workspace_size(&d, &need) != TVG_OK || !usable_beside(ws, *x, need)) return other();
+        const c10::DeviceGuard on(x->device());
+        void *stream;
+        if (!stream_handle(v[10], &stream)) return nullptr;
+        const Allocator memory(*x, v[10], stream);
+        at::Tensor dx = out ? *out : memory.result(x->sizes(), dtype);
+        at::Tensor dgamma, dbeta, scratch;
+        if (gamma) dgamma = memory.result({d.c}, at::kFloat);
+        if (beta) dbeta = memory.result({d.c}, at::kFloat);
+        if (need) scratch = enough_workspace(ws, need, memory);
+        void *dxp = dx.data_ptr(), *sp = need ? scratch.data_ptr() : nullptr;
+        const void *xp = data(x), *dyp = data(dy);
+        const float *mp = floats(mean), *rp = floats(rstd), *gp = floats(gamma), *bp = floats(beta);
+        float *dgp = gamma ? dgamma.data_ptr<float>() : nullptr, *dbp = beta ? dbeta.data_ptr<float>() : nullptr;
+        const size_t bytes = need ? bytes_of(&scratch) : 0;
+        const tvg_status st = without_gil(
+            [&] { return tvg_group_norm_fused_backward(&d, xp, dyp, mp, rp, gp, bp, dxp, dgp, dbp, sp, bytes, stream); });
+        if (st != TVG_OK) return raise_status(st, "tvg_group_norm_fused_backward");
+        const auto wrapped = [](at::Tensor &t) { return t.defined() ? THPVariable_Wrap(std::move(t)) : (Py_INCREF(Py_None), Py_None); };
+        PyObject *result = out ? (Py_INCREF(v[8]), v[8]) : THPVariable_Wrap(std::move(dx));
+        return Py_BuildValue("(NNN)", result, wrapped(dgamma), wrapped(dbeta));
+    });
+}
+
+PyObject *py_linear_lora_fused(ARGS)
+{
+    return guarded([&]() -> PyObject * {
+        PyObject *v[12];
+        if (!parse(linear_lora_fused_spec, args, nargs, kwnames, v)) return nullptr;
+        const auto other = [&] { return fall_back("linear_lora_fused", args, nargs, kwnames); };
+        if (!THPVariable_CheckExact(v[0])) return other();
+        const at::Tensor *x, *w, *a, *b, *adapter, *scale, *bias, *residual, *out, *ws;
+        int32_t act;
+        tvg_linear_lora_desc d{};
+        const c10::ScalarType dtype = THPVariable_Unpack(v[0]).scalar_type();
+        if (!plain_tensor(v[0], false, dtype, &x) || !plain_tensor(v[1], false, dtype, &w) || !plain_tensor(v[2], false, dtype, &a) ||
+            !plain_tensor(v[3], false, dtype, &b) || !plain_tensor(v[4], false, at::kInt, &adapter) ||
+            !plain_tensor(v[5], true, at::kFloat, &scale) || !plain_tensor(v[6], true, at::kFloat, &bias) ||
+            !plain_tensor(v[7], true, dtype, &residual) || !activation_code(v[8], &act) || !plain_buffer(v[9], &out) ||
+            !plain_buffer(v[10], &ws) || !known_dtype(*x, &d.dtype) || x->dim() < 1 || w->dim() != 2 || a->dim() != 3 || b->dim() != 3)
+            return other();
+        const int64_t c = x->size(-1), k = w->size(0), n = a->size(0), r = a->size(1);
+        if (c < 1 || k < 1 || n < 1 || r < 1 || x->numel() < 1 || x->numel() > INT32_MAX || k > INT32_MAX || n > INT32_MAX ||
+            r > INT32_MAX || w->size(1) != c || a->size(2) != c || b->size(0) != n || b->size(1) != k || b->size(2) != r)
+            return other();
+        const int64_t rows = x->numel() / c;
+        d.rows = (int32_t)rows; d.c = (int32_t)c; d.k = (int32_t)k; d.adapters = (int32_t)n; d.rank = (int32_t)r;
+        d.activation = act;
+        if (!beside(*x, rows, {adapter}) || !beside(*x, n, {scale}) || !beside(*x, k, {bias}) || !beside(*x, rows * k, {residual}) ||
+            w->device() != x->device() || a->device() != x->device() || b->device() != x->device() ||
+            !holds(out, *x, (size_t)(rows * k) * x->element_size()))
+            return other();
+        size_t need = 0;
+        if (tvg_linear_lora_workspace_size(&d, &need) != TVG_OK || !usable_beside(ws, *x, need)) return other();
+        const c10::DeviceGuard on(x->device());
+        void *stream;
+        if (!stream_handle(v[11], &stream)) return nullptr;
+        const Allocator memory(*x, v[11], stream);
+        at::Tensor y;
+        if (out) y = *out;
+        else {
+            c10::SmallVector<int64_t, 6> shape(x->sizes().begin(), x->sizes().end());
+            shape.back() = k;
+            y = memory.result(shape, dtype);
+        }
+        at::Tensor scratch;
+        if (need) scratch = enough_workspace(ws, need, memory);
+        void *yp = y.data_ptr(), *sp = need ? scratch.data_ptr() : nullptr;
+        const void *xp = data(x), *wp = data(w), *ap = data(a), *bp = data(b), *rp = data(residual);
+        const int32_t *ip = static_cast<const int32_t *>(data(adapter));
+        const float *scp = floats(scale), *bip = floats(bias);
+        const size_t bytes = need ? bytes_of(&scratch) : 0;
+        const tvg_status st =
+            without_gil([&] { return tvg_linear_lora_fused(&d, xp, wp, ap, bp, ip, scp, bip, rp, yp, sp, bytes, stream); });
+        if (st != TVG_OK) return raise_status(st, "tvg_linear_lora_fused");
+        if (out) {
+            Py_INCREF(v[9]);
+            return v[9];
+        }
+        return THPVariable_Wrap(std::move(y));
+    });
+}
+
+// setup(ConvDesc, TvgError, {name: Python implementation}, GroupNormDesc, LinearLoraDesc)
 PyObject *py_setup(PyObject *, PyObject *args)
 {
-    PyObject *desc, *error, *fallback;
-    if (!PyArg_ParseTuple(args, "OOO!", &desc, &error, &PyDict_Type, &fallback)) return nullptr;
+    PyObject *desc, *error, *fallback, *norm, *lora;
+    if (!PyArg_ParseTuple(args, "OOO!OO", &desc, &error, &PyDict_Type, &fallback, &norm, &lora)) return nullptr;
+    Py_INCREF(norm);
+    Py_INCREF(lora);
+    Py_XDECREF(g_norm_type);
+    Py_XDECREF(g_lora_type);
+    g_norm_type = norm;
+    g_lora_type = lora;
     Py_INCREF(desc);
     Py_INCREF(error);
     Py_INCREF(fallback);
@@ -647,7 +915,13 @@ PyMethodDef g_methods[] = {
     METHOD(conv2d_fused, "conv2d_fused($module, x, w, scale, shift, bias=None, residual=None, *, stride=1, pad=0, relu=False, out=None, workspace=None, stream=None, stream_out=False)\n--\n\ny = tail(conv2d(x, w)); allocates y (and the workspace when needed) with torch."),
     METHOD(dwconv2d_fused, "dwconv2d_fused($module, x, w, scale, shift, bias=None, residual=None, *, stride=1, pad=1, relu=False, out=None, stream=None, stream_out=False)\n--\n\ny = tail(depthwise conv2d(x, w)); allocates y with torch."),
     METHOD(dwpw_fused, "dwpw_fused($module, x, w_dw, scale_dw, shift_dw, w_pw, scale_pw, shift_pw, bias_pw=None, residual=None, *, stride=1, relu_dw=True, relu_pw=True, out=None, workspace=None, stream=None, stream_out=False, one_kernel=False)\n--\n\nMobileNet block (depthwise 3x3 + tail, 1x1 conv + tail) through tvg_dwpw_fused; allocates y with torch, and the workspace of the two-kernel form unless one_kernel asks for the form that needs none."),
-    {"setup", py_setup, METH_VARARGS, "setup(ConvDesc, TvgError, fallbacks): called once by binding.py."},
+    METHOD(tvg_group_norm_fused, "tvg_group_norm_fused($module, desc, x, gamma, beta, y, mean, rstd, workspace=None, workspace_bytes=0, stream=None)\n--\n\nThe C entry point (include/tvg.h); returns its status code."),
+    METHOD(tvg_group_norm_fused_backward, "tvg_group_norm_fused_backward($module, desc, x, dy, mean, rstd, gamma, beta, dx, dgamma, dbeta, workspace=None, workspace_bytes=0, stream=None)\n--\n\nThe C entry point (include/tvg.h); returns its status code."),
+    METHOD(tvg_linear_lora_fused, "tvg_linear_lora_fused($module, desc, x, w, a, b, adapter, scale, bias, residual, y, workspace=None, workspace_bytes=0, stream=None)\n--\n\nThe C entry point (include/tvg.h); returns its status code."),
+    METHOD(group_norm_fused, "group_norm_fused($module, x, groups, gamma=None, beta=None, *, eps=1e-5, activation=None, stats=False, out=None, workspace=None, stream=None)\n--\n\ny = act(group norm of x [n][...][c]); activation None, 'relu' or 'silu'.  With stats the result is (y, mean, rstd), which the backward call reads."),
+    METHOD(group_norm_fused_backward, "group_norm_fused_backward($module, x, dy, mean, rstd, groups, gamma=None, beta=None, *, activation=None, out=None, workspace=None, stream=None)\n--\n\n(dx, dgamma, dbeta) of group_norm_fused; dgamma and dbeta are None where gamma and beta are.  out receives dx."),
+    METHOD(linear_lora_fused, "linear_lora_fused($module, x, w, a, b, adapter, scale=None, bias=None, residual=None, *, activation=None, out=None, workspace=None, stream=None)\n--\n\ny = act(x w^T + bias + scale_i (x a_i^T) b_i^T + residual) of rows x [...][c], i = adapter of the row (int32; none where it is outside the adapters)."),
+    {"setup", py_setup, METH_VARARGS, "setup(ConvDesc, TvgError, fallbacks, GroupNormDesc, LinearLoraDesc): called once by binding.py."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "Native call path of the libtvg binding.", -1, g_methods,
@@ -668,7 +942,9 @@ PyMODINIT_FUNC PyInit__native(void)
 {
     for (const Spec *s : {&tvg_conv2d_fused_spec, &tvg_dwconv2d_fused_spec, &tvg_conv2d_fused_static_spec,
                           &tvg_conv2d_fused_dual_spec, &tvg_conv2d_fused_prepacked_spec, &tvg_dwpw_fused_spec,
-                          &tvg_maxpool2d_3x3s2_spec, &conv2d_fused_spec, &dwconv2d_fused_spec, &dwpw_fused_spec})
+                          &tvg_maxpool2d_3x3s2_spec, &conv2d_fused_spec, &dwconv2d_fused_spec, &dwpw_fused_spec,
+                          &tvg_group_norm_fused_spec, &tvg_group_norm_fused_backward_spec, &tvg_linear_lora_fused_spec,
+                          &group_norm_fused_spec, &group_norm_fused_backward_spec, &linear_lora_fused_spec})
         if (!intern(*s)) return nullptr;
     return PyModule_Create(&g_module);
 }

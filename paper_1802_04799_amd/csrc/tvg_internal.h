@@ -265,6 +265,41 @@ tvg_status launch_winograd_prepack(const ConvProblem &p, const void *w, void *pa
 tvg_status launch_conv3x3_winograd(const ConvProblem &p, const WinoPlan &plan, const void *packed,
                                    const ConvPointers &ptr, hipStream_t stream);
 
+// Group norm with an activation, channels last.
+struct NormProblem {
+    int n, p, c, groups, act, dtype;
+    float eps;
+};
+struct NormPlan {
+    int vector;                       // channels per lane
+    int block, blocks;                // channels per workgroup, workgroups across the channels
+    int rows, chunks;                 // rows per workgroup, workgroups across the rows
+    size_t lds_stats, lds_apply;
+    size_t part_floats, chan_floats;  // workspace: per group and chunk, per channel and chunk
+};
+void plan_group_norm(const NormProblem &p, int vector, NormPlan *plan);
+size_t group_norm_workspace(const NormProblem &p, bool backward);
+tvg_status launch_group_norm(const NormProblem &p, const void *x, const float *gamma, const float *beta, void *y, float *mean,
+                             float *rstd, float *workspace, hipStream_t stream);
+tvg_status launch_group_norm_backward(const NormProblem &p, const void *x, const void *dy, const float *mean, const float *rstd,
+                                      const float *gamma, const float *beta, void *dx, float *dgamma, float *dbeta,
+                                      float *workspace, hipStream_t stream);
+
+// Projection of rows with a low-rank adapter chosen row by row.
+struct LoraProblem {
+    int rows, c, k, adapters, rank, act, dtype;
+};
+struct LoraPointers {
+    const void *x, *w, *a, *b;
+    const int32_t *adapter;
+    const float *scale, *bias;
+    const void *residual;
+    void *y;
+    float *workspace;
+};
+size_t linear_lora_workspace(const LoraProblem &p);
+tvg_status launch_linear_lora(const LoraProblem &p, const LoraPointers &ptr, hipStream_t stream);
+
 tvg_status launch_conv_igemm(const ConvProblem &p, const ConvPlan &plan, const ConvPointers &ptr,
                              hipStream_t stream);
 tvg_status launch_dwconv3x3(const ConvProblem &p, const ConvPointers &ptr, hipStream_t stream);
