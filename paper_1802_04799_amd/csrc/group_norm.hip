@@ -64,16 +64,6 @@ template <typename T> struct Vec<T, 1> {
     static __device__ __forceinline__ void store(T *p, const float *f) { Elem<T>::store(p, 0, f[0]); }
 };
 
-// 1 / (1 + exp(-z)).  exp2 of z log2(e) in two parts: the product's rounding alone would cost |z| half steps.
-__device__ __forceinline__ float sigmoid(float z)
-{
-    const float c = fmaxf(z, -87.0f);                      // (exp stays finite; sigmoid is below 2^-125 there)
-    const float t = -1.44269502f * c;
-    const float lo = fmaf(-1.44269502f, c, -t) - 1.92596299e-8f * c;
-    const float e = __builtin_amdgcn_exp2f(t);
-    return __builtin_amdgcn_rcpf(1.0f + fmaf(e, 0.693147181f * lo, e));
-}
-
 template <int ACT> __device__ __forceinline__ float activate(float z)
 {
     if constexpr (ACT == TVG_ACT_RELU) return z < 0.0f ? 0.0f : z;      // (a NaN stays one)

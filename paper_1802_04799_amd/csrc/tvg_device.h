@@ -117,6 +117,16 @@ __device__ __forceinline__ float relu_floor(bool relu)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(relu ? 0u : 0x7FC00000u));
 }
 
+// 1 / (1 + exp(-z)).  exp2 of z log2(e) in two parts: the product's rounding alone would cost |z| half steps.
+__device__ __forceinline__ float sigmoid(float z)
+{
+    const float c = fmaxf(z, -87.0f);                      // (exp stays finite; sigmoid is below 2^-125 there)
+    const float t = -1.44269502f * c;
+    const float lo = fmaf(-1.44269502f, c, -t) - 1.92596299e-8f * c;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_amdgcn_rcpf(1.0f + fmaf(e, 0.693147181f * lo, e));
+}
+
 template <typename T> struct Elem;
 template <> struct Elem<float> {
     static __device__ __forceinline__ float load(const float *p, int i) { return p[i]; }
