@@ -33,6 +33,7 @@ struct LoraArgs {
     void *y;
     unsigned char *h;                      // [rows][rblocks][64 bytes]
     float *parts;                          // [splits][rows][parts_row]
+    int *order;                            // [rows]: the rows by adapter, or NULL
     int rows, c, k, adapters, rank, rblocks;
     int slots, shrink_groups;              // workgroups that share the adapters of a tile; all that make h
     int splits, chunks_per_split, parts_row;
@@ -172,19 +173,20 @@ template <typename T, int MB, int NB, int DEPTH> struct WaveProduct {
 };
 // Waves per workgroup, and as many chunks in flight as the LDS holds.
 constexpr int product_waves(int mb, int nb) { return mb + nb <= 4 ? 8 : 4; }
-constexpr int product_depth(int mb, int nb, int waves)
+constexpr int kAllLds = 152, kHalfLds = 76;                // KB that a workgroup takes: for one or two of them a CU
+constexpr int product_depth(int mb, int nb, int waves, int kb)
 {
-    const int chunks = 152 / waves / (2 * (mb + nb));      // (KB of LDS)
-    return chunks < 2 ? 2 : chunks;
+    const int chunks = kb / waves / (2 * (mb + nb));
+    return chunks < 1 ? 1 : chunks;
 }
 
 // The same for WIDE rows (whole 16-byte pieces) through LDS at `part`, and for any others.
-template <typename T, int MB, int NB, int W, bool WIDE>
+template <typename T, int MB, int NB, int W, bool WIDE, int KB>
 __device__ __forceinline__ void wave_product(const T *x0, int xrows, const T *w0, int wrows, int c, int first, int chunks, unsigned char *part,
                                              int lane, float4v (&acc)[MB][NB])
 {
     if constexpr (WIDE) {
-        WaveProduct<T, MB, NB, product_depth(MB, NB, W)> p;
+        WaveProduct<T, MB, NB, product_depth(MB, NB, W, KB)> p;
         p.start(x0, xrows, w0, wrows, (uint32_t)c * sizeof(T), part, lane);
         p.run(first, W, chunks, acc, lane);
     } else {
@@ -216,8 +218,8 @@ __device__ __forceinline__ void wave_product(const T *x0, int xrows, const T *w0
         if (i < chunks) chunk(i * 8 * E, false);
     }
 }
-template <typename T, int MB, int NB, int W, bool WIDE>
-constexpr int kPartBytes = WIDE ? WaveProduct<T, MB, NB, product_depth(MB, NB, W)>::kBytes : MB * NB * 1024;
+template <typename T, int MB, int NB, int W, bool WIDE, int KB>
+constexpr int kPartBytes = WIDE ? WaveProduct<T, MB, NB, product_depth(MB, NB, W, KB)>::kBytes : MB * NB * 1024;
 
 template <int MB, int NB> __device__ __forceinline__ void clear(float4v (&acc)[MB][NB])
 {
@@ -279,9 +281,9 @@ template <int N> __device__ __forceinline__ int distinct_adapters(const int (&mi
 
 // h of NB blocks of 16 tokens and JB blocks of 16 ranks; the waves take 128 bytes of the reduction in turn and add up through
 // LDS.  Adapters of the tile: every slots-th of them.
-template <typename T, int NB, int JB, int W, bool WIDE> __device__ __forceinline__ void shrink_tile(const LoraArgs &a, int b, unsigned char *lds)
+template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __forceinline__ void shrink_tile(const LoraArgs &a, int b, unsigned char *lds)
 {
-    constexpr int kPart = kPartBytes<T, JB, NB, W, WIDE>;
+    constexpr int kPart = kPartBytes<T, JB, NB, W, WIDE, KB>;
     static_assert(kPart >= NB * JB * 1024, "the sums lie where the chunks were");
     int *list = reinterpret_cast<int *>(lds + W * kPart), *count = list + 16 * NB;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -303,7 +305,7 @@ template <typename T, int NB, int JB, int W, bool WIDE> __device__ __forceinline
         const T *A = static_cast<const T *>(a.a) + ((size_t)i * a.rank + j0 * 16) * a.c;
         float4v acc[JB][NB];
         clear(acc);
-        wave_product<T, JB, NB, W, WIDE>(x0, a.rows - row0, A, min(a.rank - j0 * 16, 16 * JB), a.c, wave,
+        wave_product<T, JB, NB, W, WIDE, KB>(x0, a.rows - row0, A, min(a.rank - j0 * 16, 16 * JB), a.c, wave,
                                          (a.c + 8 * kPer16<T> - 1) / (8 * kPer16<T>), part, lane, acc);
         put_sums(part, lane, acc);
         __syncthreads();
@@ -330,10 +332,95 @@ template <typename T, int NB, int JB, int W, bool WIDE> __device__ __forceinline
     }
 }
 
-template <typename T, int NB, int JB, bool WIDE> __global__ __launch_bounds__(64 * product_waves(JB, NB), 2) void lora_shrink_kernel(LoraArgs a)
+// The rows in the order of their adapters (modulo kBins, rows without one last), for a product whose tiles then have few
+// adapters each.  The order of rows of an adapter is left to chance: a row's result does not depend on its place.
+constexpr int kBins = 2048, kBinsPerLane = 5;
+
+// bins[bin] += 1 for every lane with `ok`; what it was before, every lane one more than the last.  Lanes of a run add up first:
+// atomics of a wave on one address take their turns, 4096 rows of eight adapters 4 us.
+__device__ __forceinline__ int count_up(int *bins, int bin, bool ok, int lane)
+{
+    uint64_t pending = __ballot(ok);
+    int before = 0;
+    for (int round = 0; round < 4 && pending; ++round) {
+        const int first = __builtin_ctzll(pending), b = __builtin_amdgcn_readlane(bin, first);
+        const uint64_t same = __ballot(ok && bin == b) & pending;
+        int start = 0;
+        if (lane == first) start = atomicAdd(&bins[b], __popcll(same));
+        start = __builtin_amdgcn_readlane(start, first);
+        if ((same >> lane) & 1) before = start + __popcll(same & ((1ull << lane) - 1));
+        pending &= ~same;
+    }
+    if ((pending >> lane) & 1) before = atomicAdd(&bins[bin], 1);
+    return before;
+}
+
+static_assert(512 * kBinsPerLane > kBins, "a lane for every bin");
+template <int THREADS> constexpr size_t kOrderBytes = (THREADS * kBinsPerLane + THREADS / 64) * sizeof(int);
+template <int THREADS> __device__ __forceinline__ void order_rows(const LoraArgs &a, unsigned char *lds)
+{
+    int *bins = reinterpret_cast<int *>(lds), *sums = bins + THREADS * kBinsPerLane;
+    const int tid = threadIdx.x;
+    // eight rows a lane at a time: their loads are under way together
+    constexpr int kRows = 8;
+    const auto bins_of = [&](int r0, int (&bin)[kRows]) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) bin[u] = a.adapter[min(r0 + u * THREADS + tid, a.rows - 1)];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) bin[u] = bin[u] < 0 || bin[u] >= a.adapters ? kBins : bin[u] % kBins;
+    };
+    for (int i = tid; i < THREADS * kBinsPerLane; i += THREADS) bins[i] = 0;
+    __syncthreads();
+    int bin[kRows];
+    for (int r0 = 0; r0 < a.rows; r0 += kRows * THREADS) {
+        bins_of(r0, bin);
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            count_up(bins, bin[u], r0 + u * THREADS + tid < a.rows, tid & 63);
+    }
+    __syncthreads();
+    int mine[kBinsPerLane], total = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsPerLane; ++i) {
+        mine[i] = total;
+        total += bins[tid * kBinsPerLane + i];
+    }
+    // sums of the lanes before: within the wave, then of the waves
+    int upto = total;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int v = __shfl_up(upto, d);
+        upto += (tid & 63) >= d ? v : 0;
+    }
+    if ((tid & 63) == 63) sums[tid >> 6] = upto;
+    __syncthreads();
+    for (int w = 0; w < tid >> 6; ++w) upto += sums[w];
+    const int before = upto - total;
+#pragma unroll
+    for (int i = 0; i < kBinsPerLane; ++i) bins[tid * kBinsPerLane + i] = before + mine[i];
+    __syncthreads();
+    for (int r0 = 0; r0 < a.rows; r0 += kRows * THREADS) {
+        if (a.rows > kRows * THREADS) bins_of(r0, bin);
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int r = r0 + u * THREADS + tid;
+            const int at = count_up(bins, bin[u], r < a.rows, tid & 63);
+            if (r < a.rows) a.order[at] = r;
+        }
+    }
+}
+
+// The first workgroup orders the rows where that is wanted, the others make h.  Two a CU, since with it they are one more than
+// the CUs where tiles are as many.
+constexpr int kShrinkWaves = 8;
+template <typename T, int NB, int JB, bool WIDE> __global__ __launch_bounds__(64 * kShrinkWaves, 2) void lora_shrink_kernel(LoraArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    shrink_tile<T, NB, JB, product_waves(JB, NB), WIDE>(a, blockIdx.x, lds);
+    if (a.order && blockIdx.x == 0) {
+        order_rows<64 * kShrinkWaves>(a, lds);
+        return;
+    }
+    shrink_tile<T, NB, JB, kShrinkWaves, WIDE, kHalfLds>(a, blockIdx.x - (a.order ? 1 : 0), lds);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -381,13 +468,13 @@ __device__ __forceinline__ float lora_act(float t, int act)
 }
 
 // Stores a wave's accumulators through LDS of its own, with the tail: whole rows of the tile's channels leave as 16-byte
-// stores, or element by element where rows of y do not allow it.  Two blocks of 16 tokens at a time, in loops that stay
+// stores, or element by element where rows of y do not allow it (row_of: the rows of the wave's tokens).  Two blocks of 16 tokens at a time, in loops that stay
 // loops: code that runs once a tile is fetched once a tile.
 constexpr int kStoreTokens = 32;
 template <int MB> constexpr int kStoreRow = 16 * MB + 4;   // floats; the four keep rows on different banks
 template <int MB> constexpr int kStoreBytes = kStoreTokens * kStoreRow<MB> * 4;
 template <typename T, int MB, int NB>
-__device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, int row0, int lane, const float4v (&acc)[MB][NB], float *stage)
+__device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, const int *row_of, int lane, const float4v (&acc)[MB][NB], float *stage)
 {
     static_assert(NB % 2 == 0, "two blocks of tokens at a time");
     constexpr int kRow = kStoreRow<MB>, E = kPer16<T>;
@@ -414,7 +501,7 @@ __device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, int 
         if (wide) {
 #pragma unroll 1
             for (int t = lane / kLanes; t < kStoreTokens; t += kTokens) {
-                const int row = row0 + n * 16 + t;
+                const int row = row_of[n * 16 + t];
                 if (row >= a.rows || c16 >= a.k) break;
                 const size_t at = (size_t)row * a.k + c16;
                 float f[E];
@@ -447,7 +534,7 @@ __device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, int 
         } else {
 #pragma unroll 1
             for (int t = lane / kLanes1; t < kStoreTokens; t += kTokens1) {
-                const int row = row0 + n * 16 + t;
+                const int row = row_of[n * 16 + t];
                 if (row >= a.rows || c1 >= a.k) break;
                 const size_t at = (size_t)row * a.k + c1;
                 float f = stage[t * kRow + lane % kLanes1] + bias[0];
@@ -534,7 +621,7 @@ template <typename T> __device__ __forceinline__ void store4(const LoraArgs &a, 
 enum { kAnyRows = 0, kWideRows = 1, kParts = 2 };
 template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bounds__(64 * W, 2) void linear_lora_waves_kernel(LoraArgs a)
 {
-    constexpr int kPart = MODE == kWideRows ? kPartBytes<T, MB, NB, W, true> : MB * NB * 1024;
+    constexpr int kPart = MODE == kWideRows ? kPartBytes<T, MB, NB, W, true, kAllLds> : MB * NB * 1024;
     static_assert(kPart >= NB * MB * 1024, "the sums lie where the chunks were");
     extern __shared__ __align__(16) unsigned char lds[];
     const int tile = xcd_remap(blockIdx.x, a.tiles);
@@ -557,7 +644,7 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
                         acc[m][n] += *reinterpret_cast<const float4v *>(a.parts + ((size_t)s * a.rows + row) * a.parts_row + ch0 + m * 16 + quad * 4);
                 }
     } else {
-        wave_product<T, MB, NB, W, MODE == kWideRows>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
+        wave_product<T, MB, NB, W, MODE == kWideRows, kAllLds>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
                                                       static_cast<const T *>(a.w) + (size_t)ch0 * a.c, a.k - ch0, a.c, wave,
                                                       (a.c + 8 * kPer16<T> - 1) / (8 * kPer16<T>), part, lane, acc);
     }
@@ -572,10 +659,10 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
 // reduction, which the next launch adds up.
 template <typename T, int MB, int NB, bool WIDE> __global__ __launch_bounds__(64 * product_waves(MB, NB), 2) void lora_parts_kernel(LoraArgs a)
 {
-    constexpr int W = product_waves(MB, NB), kPart = kPartBytes<T, MB, NB, W, WIDE>;
+    constexpr int W = product_waves(MB, NB), kPart = kPartBytes<T, MB, NB, W, WIDE, kAllLds>;
     extern __shared__ __align__(16) unsigned char lds[];
     if ((int)blockIdx.x < a.shrink_groups) {
-        shrink_tile<T, 1, 1, W, WIDE>(a, blockIdx.x, lds);
+        shrink_tile<T, 1, 1, W, WIDE, kAllLds>(a, blockIdx.x, lds);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -589,7 +676,7 @@ template <typename T, int MB, int NB, bool WIDE> __global__ __launch_bounds__(64
     clear(acc);
     unsigned char *part = lds + wave * kPart;
     const int chunks = (a.c + 8 * kPer16<T> - 1) / (8 * kPer16<T>);
-    wave_product<T, MB, NB, W, WIDE>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
+    wave_product<T, MB, NB, W, WIDE, kAllLds>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
                                      static_cast<const T *>(a.w) + (size_t)ch0 * a.c, a.k - ch0, a.c, split * a.chunks_per_split + wave,
                                      min(chunks, (split + 1) * a.chunks_per_split), part, lane, acc);
     put_sums(part, lane, acc);
@@ -610,7 +697,7 @@ template <typename K> bool allow_lds(K kernel, size_t bytes)
 template <typename T, int MB, int NB, int W, int MODE> tvg_status launch_waves(LoraArgs a, hipStream_t stream)
 {
     const auto kernel = linear_lora_waves_kernel<T, MB, NB, W, MODE>;
-    constexpr size_t kLds = (size_t)W * (MODE == kWideRows ? kPartBytes<T, MB, NB, W, true> : MB * NB * 1024);
+    constexpr size_t kLds = (size_t)W * (MODE == kWideRows ? kPartBytes<T, MB, NB, W, true, kAllLds> : MB * NB * 1024);
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     a.tiles_n = (a.k + 16 * MB - 1) / (16 * MB);
@@ -623,7 +710,7 @@ template <typename T, int MB, int NB, bool WIDE> tvg_status launch_parts(LoraArg
 {
     const auto kernel = lora_parts_kernel<T, MB, NB, WIDE>;
     constexpr int W = product_waves(MB, NB);
-    constexpr size_t kLds = std::max((size_t)W * kPartBytes<T, MB, NB, W, WIDE>, (size_t)W * kPartBytes<T, 1, 1, W, WIDE> + 17 * sizeof(int));
+    constexpr size_t kLds = std::max((size_t)W * kPartBytes<T, MB, NB, W, WIDE, kAllLds>, (size_t)W * kPartBytes<T, 1, 1, W, WIDE, kAllLds> + 17 * sizeof(int));
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     a.tiles_n = (a.k + 16 * MB - 1) / (16 * MB);
@@ -653,7 +740,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
     static_assert(kLoads * W * 16 == TM + TN && kLoadsX * W * 16 == TM, "every wave loads whole rows of one operand");
     static_assert(MB <= 4 && W * kStoreBytes<MB> <= RING * kStage, "the stores' rows lie where the ring was");
     extern __shared__ __align__(1024) unsigned char lds[];
-    int *ids = reinterpret_cast<int *>(lds + RING * kStage), *list = ids + TM;
+    int *row_of = reinterpret_cast<int *>(lds + RING * kStage), *ids = row_of + TM, *list = ids + TM;
     const int tile = xcd_remap(blockIdx.x, a.tiles);
     int tm, tn;
     {
@@ -667,7 +754,9 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
     const int rsel = lane & 15, quad = lane >> 4;
     const int row0 = tm * TM, ch0 = tn * TN, wr = wave % WR * (TM / WR), wc = wave / WR * (TN / WC);
     const uint32_t row_bytes = (uint32_t)a.c * sizeof(T);
-    const uint4v xbuf = raw_buffer(static_cast<const T *>(a.x) + (size_t)row0 * a.c, (uint32_t)min(TM, a.rows - row0) * row_bytes);
+    // (rows in order of their adapters: anywhere in x, whose bytes 32 bits count then)
+    const int base = a.order ? 0 : row0, reach = a.order ? a.rows : min(TM, a.rows - row0);
+    const uint4v xbuf = raw_buffer(static_cast<const T *>(a.x) + (size_t)base * a.c, (uint32_t)reach * row_bytes);
     const uint4v wbuf = raw_buffer(static_cast<const T *>(a.w) + (size_t)ch0 * a.c, (uint32_t)min(TN, a.k - ch0) * row_bytes);
     // a load: 16 rows of an operand; where a lane's 16 bytes come from
     uint32_t from[kLoads];
@@ -676,17 +765,25 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
     for (int i = 0; i < kLoads; ++i) {
         const int block = i < kLoadsX ? i * W + wave : (i - kLoadsX) * W + wave;
         const int row = block * 16 + lrow, end = i < kLoadsX ? min(TM, a.rows - row0) : min(TN, a.k - ch0);
-        from[i] = row < end ? row * row_bytes + piece * 16 : kBeyond;
+        const uint32_t at = i < kLoadsX && a.order && row < end ? a.order[row0 + row] : row;
+        from[i] = row < end ? at * row_bytes + piece * 16 : kBeyond;
     }
     const int whole = (int)(row_bytes / kSlice), steps = (int)((row_bytes + kSlice - 1) / kSlice);
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)lds);
     const int turns = (steps + 1) & ~1;                    // (an odd step more: zeros)
-    int plain = turns;                                     // steps that every token takes: all, where the tile has one adapter
-    int fetched = 0, fetched_block = 0, adapters = 0;      // the adapter, its block of ranks that comes next; how many there are
+    int adapters = 0, blocks = 0, fetched = 0;             // of the tile; blocks of ranks in the ring, the next one
     const auto fetch = [&](int s) {                        // a whole slice of the channels
         const uint32_t to = lds0 + (s & (RING - 1)) * kStage + wave * 1024;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load_to_lds(to + i * W * 1024, from[i], i < kLoadsX ? xbuf : wbuf, s * kSlice);
+    };
+    // 16 bytes a lane of a row of B at any element: through registers (whose loads are younger than the step's own, and waited for)
+    const auto copy_b = [&](int i, int row, int r0, int to) {
+        const T *from_b = static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0 + row) * a.rank + r0;
+        T *to_b = reinterpret_cast<T *>(lds + to + lane * 16);
+#pragma unroll 1
+        for (int e = 0; e < kPer16<T>; ++e) to_b[e] = ch0 + row < a.k && r0 + e < a.rank ? from_b[e] : (T)0;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
     const auto fetch_any = [&](int s) {
         const uint32_t to = lds0 + (s & (RING - 1)) * kStage + wave * 1024;
@@ -698,36 +795,24 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
             }
             return;
         }
-        // a block of 16 ranks: h of the tokens, and B, whose 16 ranks bf16 takes twice
-        const bool any = fetched < adapters;
-        const int i = any ? __builtin_amdgcn_readfirstlane(list[fetched]) : 0;
-        const uint4v hbuf = raw_buffer(a.h + (size_t)row0 * a.rblocks * 64, (uint32_t)min(TM, a.rows - row0) * a.rblocks * 64);
+        // a block of 16 ranks of the only adapter: h of the tokens, and B, whose 16 ranks bf16 takes twice
+        const bool any = fetched < blocks;
+        const int i = any ? __builtin_amdgcn_readfirstlane(list[0]) : 0;
+        const uint4v hbuf = raw_buffer(a.h + (size_t)base * a.rblocks * 64, (uint32_t)reach * a.rblocks * 64);
         const uint4v bbuf = raw_buffer(static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0) * a.rank,
                                        (uint32_t)min(TN, a.k - ch0) * a.rank * (uint32_t)sizeof(T));
-        const uint32_t bpiece = sizeof(T) == 2 ? fetched_block * 32 + (piece & 1) * 16 : fetched_block * 64 + piece * 16;
+        const uint32_t bpiece = sizeof(T) == 2 ? fetched * 32 + (piece & 1) * 16 : fetched * 64 + piece * 16;
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int row = (n < kLoadsX ? n * W + wave : (n - kLoadsX) * W + wave) * 16 + lrow;
             const int end = n < kLoadsX ? min(TM, a.rows - row0) : min(TN, a.k - ch0);
-            uint32_t at = n < kLoadsX ? (row * a.rblocks + fetched_block) * 64 + piece * 16
+            uint32_t at = n < kLoadsX ? ((row_of[row & (TM - 1)] - base) * a.rblocks + fetched) * 64 + piece * 16
                                       : row * a.rank * (uint32_t)sizeof(T) + bpiece;
             if (!any || row >= end || (n >= kLoadsX && bpiece >= a.rank * sizeof(T))) at = kBeyond;
-            if (n < kLoadsX || a.wide_rank || !any) {
-                load_to_lds(to + n * W * 1024, at, n < kLoadsX ? hbuf : bbuf, 0);
-                continue;
-            }
-            // rows of B at any element: through registers (whose loads are younger than this step's own, and waited for)
-            const int r0 = (int)(bpiece / sizeof(T));
-            const T *from_b = static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0 + row) * a.rank + r0;
-            T *to_b = reinterpret_cast<T *>(lds + (to - lds0) + n * W * 1024 + lane * 16);
-#pragma unroll 1
-            for (int e = 0; e < kPer16<T>; ++e) to_b[e] = row < end && r0 + e < a.rank ? from_b[e] : (T)0;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (n < kLoadsX || a.wide_rank || !any) load_to_lds(to + n * W * 1024, at, n < kLoadsX ? hbuf : bbuf, 0);
+            else copy_b(i, row, (int)(bpiece / sizeof(T)), (int)(to - lds0) + n * W * 1024);
         }
-        if (++fetched_block == a.rblocks) {
-            fetched_block = 0;
-            ++fetched;
-        }
+        ++fetched;
     };
     float4v acc[MB][NB];
 #pragma unroll
@@ -761,14 +846,19 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    for (int t = threadIdx.x; t < TM; t += 64 * W)
+        row_of[t] = row0 + t >= a.rows ? a.rows : a.order ? a.order[row0 + t] : row0 + t;
 #pragma unroll 1
     for (int i = 0; i < RING - 1; ++i) {
         if (i == 2 && a.adapters > 0) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
             if (wave == 0) {
                 constexpr int N = (TM + 63) / 64;
                 int mine[N];
 #pragma unroll
-                for (int n = 0; n < N; ++n) mine[n] = adapter_of(a, row0 + n * 64 + lane);
+                for (int n = 0; n < N; ++n) mine[n] = adapter_of(a, row_of[n * 64 + lane]);
                 const int found = distinct_adapters<N>(mine, lane, list);
                 const int first = found ? list[0] : -1;
                 bool same = true;
@@ -787,7 +877,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             adapters = __builtin_amdgcn_readfirstlane(list[TM]);
-            plain = __builtin_amdgcn_readfirstlane(list[TM + 1]) ? turns + adapters * a.rblocks : turns;
+            if (__builtin_amdgcn_readfirstlane(list[TM + 1])) blocks = adapters * a.rblocks;
         }
         fetch_any(i);
     }
@@ -800,41 +890,81 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         step(s, xv[0], wv[0], xv[1], wv[1]);
         step(s + 1, xv[1], wv[1], xv[0], wv[0]);
     }
-    // the last slices, then the adapters' blocks of ranks
-    const int end = turns + adapters * a.rblocks;
-    int at = 0, block = 0;
-    // (two loops: as branches of one, their accumulators do not get the same registers)
+    // the last slices, then, where all tokens have the same adapter, its blocks of ranks
 #pragma unroll 1
-    for (; s < plain; ++s) {
+    for (const int end = turns + blocks; s < end; ++s) {
         behind();
         fetch_any(s + RING - 1);
         read(s, xv[0], wv[0]);
         multiply(xv[0], wv[0]);
     }
-#pragma unroll 1
-    for (; s < end; ++s) {
-        behind();
-        fetch_any(s + RING - 1);
-        const unsigned char *p = lds + (s & (RING - 1)) * kStage;
+    if (adapters > 0 && blocks == 0) {
+        // Several adapters: a block of ranks of h stays in registers while B of every adapter comes through the ring, deeper
+        // than before since it is B alone.
+        constexpr int kRow = sizeof(T) == 2 && TN > 64 ? 32 : 64;      // bytes of a row of B (bf16, 64: its 16 ranks twice)
+        constexpr int kBLoads = TN * kRow / 1024 / W, kBStage = TN * kRow, kBRing = 8;
+        static_assert(kBLoads * W * 1024 == TN * kRow && kBRing * kBStage <= RING * kStage, "whole loads of every wave, in the ring's place");
+        const int total = adapters * a.rblocks;
+        int next = 0, next_at = 0, next_block = 0;
+        const auto fetch_b = [&] {
+            const bool any = next < total;
+            const int i = any ? __builtin_amdgcn_readfirstlane(list[next_at]) : 0;
+            const uint4v bbuf = raw_buffer(static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0) * a.rank,
+                                           (uint32_t)min(TN, a.k - ch0) * a.rank * (uint32_t)sizeof(T));
+            const uint32_t to = (next & (kBRing - 1)) * kBStage + wave * 1024;
 #pragma unroll
-        for (int m = 0; m < MB; ++m) wv[0][m] = *reinterpret_cast<const uint4v *>(p + wat + m * 16 * kSlice);
-        const int i = __builtin_amdgcn_readfirstlane(list[at]);
-        multiply_adapter<T>([&](int n) { return ids[wr + n * 16 + rsel] == i; }, wv[0],
-                            [&](int n) { return *reinterpret_cast<const uint4v *>(p + xat + n * 16 * kSlice); }, acc);
-        if (++block == a.rblocks) {
-            block = 0;
-            ++at;
+            for (int l = 0; l < kBLoads; ++l) {
+                const int byte = (l * W + wave) * 1024 + lane * 16, row = byte / kRow;
+                const uint32_t r = sizeof(T) == 2 ? next_block * 32 + (lane & 1) * 16 : next_block * 64 + (lane & 3) * 16;
+                const bool ok = any && ch0 + row < a.k && r < a.rank * sizeof(T);
+                if (a.wide_rank || !any) load_to_lds(lds0 + to + l * W * 1024, ok ? row * a.rank * (uint32_t)sizeof(T) + r : kBeyond, bbuf, 0);
+                else copy_b(i, row, (int)(r / sizeof(T)), (int)to + l * W * 1024);
+            }
+            ++next;
+            if (++next_at == adapters) {
+                next_at = 0;
+                ++next_block;
+            }
+        };
+        wait_loads<0>();
+        __builtin_amdgcn_s_barrier();                      // (all waves have read the ring)
+        asm volatile("" ::: "memory");
+#pragma unroll 1
+        for (int d = 0; d < kBRing - 1; ++d) fetch_b();
+        int mine[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) mine[n] = ids[wr + n * 16 + rsel];
+        const int bat = (wc + rsel) * kRow + (sizeof(T) == 2 ? quad & 1 : quad) * 16;
+        int e = 0;
+#pragma unroll 1
+        for (int j = 0; j < a.rblocks; ++j) {
+            uint4v hv[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) hv[n] = load_h(a, min(row_of[wr + n * 16 + rsel], a.rows - 1), j, quad);
+#pragma unroll 1
+            for (int at = 0; at < adapters; ++at, ++e) {
+                wait_loads<(kBRing - 2) * kBLoads>();
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                fetch_b();
+                const int i = __builtin_amdgcn_readfirstlane(list[at]);
+                const unsigned char *p = lds + (e & (kBRing - 1)) * kBStage + bat;
+                uint4v bv[MB];
+#pragma unroll
+                for (int m = 0; m < MB; ++m) bv[m] = *reinterpret_cast<const uint4v *>(p + m * 16 * kRow);
+                multiply_adapter<T>([&](int n) { return mine[n] == i; }, bv, [&](int n) { return hv[n]; }, acc);
+            }
         }
     }
     wait_loads<0>();
     __syncthreads();
-    store_rows<T, MB, NB>(a, ch0 + wc, row0 + wr, lane, acc, reinterpret_cast<float *>(lds + wave * kStoreBytes<MB>));
+    store_rows<T, MB, NB>(a, ch0 + wc, row_of + wr, lane, acc, reinterpret_cast<float *>(lds + wave * kStoreBytes<MB>));
 }
 
 template <typename T, int TM, int TN, int WR, int WC, int RING> tvg_status launch_tile(LoraArgs a, hipStream_t stream)
 {
     const auto kernel = linear_lora_tile_kernel<T, TM, TN, WR, WC, RING>;
-    constexpr size_t kLds = (size_t)RING * (TM + TN) * kSlice + (2 * TM + 2) * sizeof(int);
+    constexpr size_t kLds = (size_t)RING * (TM + TN) * kSlice + (3 * TM + 2) * sizeof(int);
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     a.tiles_n = (a.k + TN - 1) / TN;
@@ -848,14 +978,14 @@ int rank_blocks(const LoraProblem &p) { return (p.rank + 15) / 16; }
 template <typename T, int NB, int JB, bool WIDE> tvg_status launch_shrink(LoraArgs a, hipStream_t stream)
 {
     const auto kernel = lora_shrink_kernel<T, NB, JB, WIDE>;
-    constexpr int W = product_waves(JB, NB);
-    constexpr size_t kLds = (size_t)W * kPartBytes<T, JB, NB, W, WIDE> + (16 * NB + 1) * sizeof(int);
+    constexpr int W = kShrinkWaves;
+    constexpr size_t kLds = std::max((size_t)W * kPartBytes<T, JB, NB, W, WIDE, kHalfLds> + (16 * NB + 1) * sizeof(int), kOrderBytes<64 * W>);
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     const int tiles = (a.rows + 16 * NB - 1) / (16 * NB) * ((a.rblocks + JB - 1) / JB);
     // few tiles: their adapters in turn by several workgroups
-    a.slots = std::max(1, std::min(std::min(16 * NB, std::min(a.rows, a.adapters)), kComputeUnits / tiles));
-    hipLaunchKernelGGL(kernel, dim3(tiles * a.slots), dim3(64 * W), kLds, stream, a);
+    a.slots = std::max(1, std::min(std::min(16 * NB, std::min(a.rows, a.adapters)), 2 * kComputeUnits / tiles));
+    hipLaunchKernelGGL(kernel, dim3(tiles * a.slots + (a.order ? 1 : 0)), dim3(64 * W), kLds, stream, a);
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
@@ -879,7 +1009,7 @@ PartsPlan plan_parts(const LoraProblem &p, bool wide)
     PartsPlan plan{};
     plan.parts_row = (p.k + 63) / 64 * 64;
     plan.h_bytes = p.adapters > 0 ? ((size_t)p.rows * rank_blocks(p) * 64 + 255) & ~(size_t)255 : 0;
-    plan.bytes = plan.h_bytes;
+    plan.bytes = plan.h_bytes + (p.adapters > 0 ? (size_t)p.rows * sizeof(int) : 0);
     plan.use = tiles_of(p, 64, 64) < kComputeUnits;
     if (!plan.use) return plan;
     const int chunks = (int)(((size_t)p.c * (p.dtype == TVG_BF16 ? 2 : 4) + 127) / 128);
@@ -894,7 +1024,7 @@ PartsPlan plan_parts(const LoraProblem &p, bool wide)
     const int splits = std::max(1, std::min(most(), (kComputeUnits - htiles * plan.slots) / tiles));
     plan.chunks_per_split = (chunks + splits - 1) / splits;
     plan.splits = (chunks + plan.chunks_per_split - 1) / plan.chunks_per_split;
-    plan.bytes += (size_t)plan.splits * p.rows * plan.parts_row * sizeof(float);
+    plan.bytes = plan.h_bytes + (size_t)plan.splits * p.rows * plan.parts_row * sizeof(float);
     return plan;
 }
 
@@ -931,6 +1061,8 @@ template <typename T> tvg_status launch(const LoraProblem &p, LoraArgs &a, hipSt
     const PartsPlan parts = plan_parts(p, wide);
     if (parts.use) return launch_few_tiles<T>(parts, wide, a, stream);
     if (p.adapters > 0) {
+        if (wide && (int64_t)p.rows * std::max((int64_t)p.c * (int64_t)sizeof(T), (int64_t)a.rblocks * 64) < (int64_t)kBeyond)
+            a.order = reinterpret_cast<int *>(a.h + parts.h_bytes);
         const tvg_status st = !wide ? launch_shrink<T, 1, 1, false>(a, stream)
                                     : a.rblocks == 1 ? launch_shrink<T, 1, 1, true>(a, stream) : launch_shrink<T, 2, 2, true>(a, stream);
         if (st != TVG_OK) return st;
