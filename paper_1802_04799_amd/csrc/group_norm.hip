@@ -18,6 +18,7 @@
 //   mean = mean_a + d n_b / n,  M2 = M2_a + M2_b + d^2 n_a n_b / n,  d = mean_b - mean_a.
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "tvg_device.h"
 #include "tvg_internal.h"
@@ -93,6 +94,7 @@ struct NormArgs {
     int n, p, c, groups, cpg, block, blocks, rows, chunks;      // channels per block, rows per chunk
     int tiles;                             // n * blocks * chunks
     float eps;
+    int act;
 };
 
 // The part of the problem that a workgroup has.
@@ -116,11 +118,39 @@ template <int V> __device__ __forceinline__ Tile tile_of(const NormArgs &a, int 
 }
 
 // Sum over the lanes of a team; the result in all of them.
-__device__ __forceinline__ float team_sum(float v)
+template <int TEAM = kTeam> __device__ __forceinline__ float team_sum(float v)
 {
 #pragma unroll
-    for (int d = 1; d < kTeam; d *= 2) v += __shfl_xor(v, d, kTeam);
+    for (int d = 1; d < TEAM; d *= 2) v += __shfl_xor(v, d, TEAM);
     return v;
+}
+
+// f(i, group) for the channels cc + i of a lane, groups counted from the block's first.
+template <int V, bool WHOLE, typename F> __device__ __forceinline__ void for_channels(int cc, int cpg, F &&f)
+{
+    int c;
+    int g = fast_div(cc, cpg, 1.0f / (float)cpg, &c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        f(i, g);
+        if constexpr (!WHOLE) {
+            const bool next = ++c == cpg;
+            g += next;
+            c = next ? 0 : c;
+        }
+    }
+}
+
+// The pairs of a group's chunks, eight lanes a group: all loads of a lane are under way together.
+constexpr int kPairTeam = 8, kPairs = 64 / kPairTeam;
+__device__ __forceinline__ void load_pairs(const NormArgs &a, int sample, int group, int tl, float2 (&v)[kPairs])
+{
+    const float2 *part = reinterpret_cast<const float2 *>(a.part) + ((size_t)sample * a.groups + group) * a.chunks;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const int k = tl + i * kPairTeam;
+        v[i] = k < a.chunks ? part[k] : float2{0.0f, 0.0f};
+    }
 }
 
 // U rows of a lane's channels joined to its running mean and M2 of `count` rows (rows beyond `left` do not count).
@@ -162,14 +192,15 @@ __device__ __forceinline__ void join_rows(const typename Vec<T, V>::type (&raw)[
 }
 
 // LDS: per channel of a pass the lanes' (mean, M2, rows), then per group (elements, mean, M2).
-template <typename T, int V> __global__ __launch_bounds__(kThreads) void group_norm_stats_kernel(NormArgs a)
+template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_stats_kernel(NormArgs a)
 {
-    constexpr int U = 8;
+    constexpr int U = 8, Q = WHOLE ? 1 : V;                // entries per lane
     extern __shared__ float lds[];
-    float *lane_mean = lds, *lane_m2 = lds + kThreads * V, *group = lds + 2 * kThreads * V;
+    float *lane_mean = lds, *lane_m2 = lds + kThreads * Q, *group = lds + 2 * kThreads * Q;
     const Tile t = tile_of<V>(a, blockIdx.x);
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
-    const int col = threadIdx.x % t.cols, rp = threadIdx.x / t.cols;
+    int col;
+    const int rp = fast_div(threadIdx.x, t.cols, 1.0f / (float)t.cols, &col);
     const T *x = static_cast<const T *>(a.x) + ((size_t)t.sample * a.p) * a.c + t.c0;
     for (int g = threadIdx.x; g < ng; g += kThreads) group[3 * g] = group[3 * g + 1] = group[3 * g + 2] = 0.0f;
     for (int pass = 0; pass * t.cols * V < t.width; ++pass) {
@@ -197,30 +228,51 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void group_n
             }
         }
         __syncthreads();                                   // (the previous pass has been read)
+        if constexpr (WHOLE) {                             // the lane's channels are of one group
+            float m = 0.0f, q = 0.0f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            lane_mean[threadIdx.x * V + i] = mean[i];
-            lane_m2[threadIdx.x * V + i] = m2[i];
+            for (int i = 0; i < V; ++i) m += mean[i];
+            m *= 1.0f / V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = mean[i] - m;
+                q += fmaf(d * d, (float)count, m2[i]);
+            }
+            lane_mean[threadIdx.x] = m;
+            lane_m2[threadIdx.x] = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                lane_mean[threadIdx.x * V + i] = mean[i];
+                lane_m2[threadIdx.x * V + i] = m2[i];
+            }
         }
         __syncthreads();
-        // a team joins the entries of a group's channels in this pass: rp lanes per channel, of known row counts
-        const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
+        // a team joins the entries of a group in this pass: rp lanes per column, of known row counts
+        constexpr int P = V / Q;                           // channels per entry
+        const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam, row_entries = t.cols * Q;
         for (int g = first / a.cpg + team; g * a.cpg < first + pass_width; g += kThreads / kTeam) {
-            const int lo = max(g * a.cpg, first), hi = min((g + 1) * a.cpg, first + pass_width), w = hi - lo;
+            const int lo = max(g * a.cpg, first), hi = min((g + 1) * a.cpg, first + pass_width);
+            const int base = (lo - first) / P, w = (hi - lo) / P;
             const int entries = w * t.rp, rows = t.row1 - t.row0;
+            const float inv_w = 1.0f / (float)w, inv_rp = 1.0f / (float)t.rp;
+            const auto rows_of = [&](int r) {              // rows of a lane: every rp-th
+                int rest;
+                return r < rows ? fast_div(rows - r + t.rp - 1, t.rp, inv_rp, &rest) : 0;
+            };
             float s = 0.0f;
             for (int e = tl; e < entries; e += kTeam) {
-                const int r = e / w, at = r * t.cols * V + lo - first + e - r * w;
-                const int n = r < rows ? (rows - r + t.rp - 1) / t.rp : 0;
-                s += (float)n * lane_mean[at];
+                int c;
+                const int r = fast_div(e, w, inv_w, &c);
+                s += (float)rows_of(r) * lane_mean[r * row_entries + base + c];
             }
-            const float total = (float)rows * (float)w, m = team_sum(s) / total;
+            const float m = team_sum(s) / ((float)rows * (float)w), total = (float)rows * (float)(w * P);
             float q = 0.0f;
             for (int e = tl; e < entries; e += kTeam) {
-                const int r = e / w, at = r * t.cols * V + lo - first + e - r * w;
-                const int n = r < rows ? (rows - r + t.rp - 1) / t.rp : 0;
+                int c;
+                const int r = fast_div(e, w, inv_w, &c), at = r * row_entries + base + c, n = rows_of(r);
                 const float d = lane_mean[at] - m;
-                q += n ? fmaf(d * d, (float)n, lane_m2[at]) : 0.0f;
+                q += n ? fmaf(d * d, (float)(n * P), lane_m2[at]) : 0.0f;
             }
             q = team_sum(q);
             if (tl == 0) {
@@ -243,19 +295,22 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void group_n
 // Mean and 1/sqrt(var + eps) of the tile's groups from the chunks' partial statistics, into LDS.
 __device__ __forceinline__ void join_chunks(const NormArgs &a, const Tile &t, int g0, int ng, float *gmean, float *grstd)
 {
-    const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
+    const int team = threadIdx.x / kPairTeam, tl = threadIdx.x % kPairTeam;
     const float total = (float)a.p;                        // (in rows: every chunk has cpg channels a row)
-    for (int g = team; g < ng; g += kThreads / kTeam) {
-        const float *part = a.part + ((size_t)t.sample * a.groups + g0 + g) * a.chunks * 2;
+    for (int g = team; g < ng; g += kThreads / kPairTeam) {
+        float2 v[kPairs];
+        load_pairs(a, t.sample, g0 + g, tl, v);
         float s = 0.0f;
-        for (int k = tl; k < a.chunks; k += kTeam) s += (float)min(a.rows, a.p - k * a.rows) * part[2 * k];
-        const float m = team_sum(s) / total;
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) s += (float)max(0, min(a.rows, a.p - (tl + i * kPairTeam) * a.rows)) * v[i].x;
+        const float m = team_sum<kPairTeam>(s) / total;
         float q = 0.0f;
-        for (int k = tl; k < a.chunks; k += kTeam) {
-            const float d = part[2 * k] - m;
-            q += fmaf(d * d, (float)min(a.rows, a.p - k * a.rows) * (float)a.cpg, part[2 * k + 1]);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const float d = v[i].x - m, n = (float)max(0, min(a.rows, a.p - (tl + i * kPairTeam) * a.rows)) * (float)a.cpg;
+            q += n > 0.0f ? fmaf(d * d, n, v[i].y) : 0.0f;
         }
-        q = team_sum(q);
+        q = team_sum<kPairTeam>(q);
         if (tl == 0) {
             const float r = 1.0f / sqrtf(q / (total * (float)a.cpg) + a.eps);
             gmean[g] = m;
@@ -266,69 +321,90 @@ __device__ __forceinline__ void join_chunks(const NormArgs &a, const Tile &t, in
     }
 }
 
-template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) void group_norm_apply_kernel(NormArgs a)
+template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_apply_kernel(NormArgs a)
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
     const Tile t = tile_of<V>(a, blockIdx.x);
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
     float *gmean = lds, *grstd = lds + ng;
-    join_chunks(a, t, g0, ng, gmean, grstd);
-    __syncthreads();
-    const int col = threadIdx.x % t.cols, rp = threadIdx.x / t.cols;
-    if (rp >= t.rp) return;
+    int col;
+    const int rp = fast_div(threadIdx.x, t.cols, 1.0f / (float)t.cols, &col);
     const T *x = static_cast<const T *>(a.x) + ((size_t)t.sample * a.p) * a.c + t.c0;
     T *y = static_cast<T *>(a.y) + ((size_t)t.sample * a.p) * a.c + t.c0;
-    for (int cc = col * V; cc < t.width; cc += t.cols * V) {
+    bool joined = false;
+    for (int cc = col * V, pass = 0; pass * t.cols * V < t.width; ++pass, cc += t.cols * V) {
+        const bool active = rp < t.rp && cc < t.width;
+        // the first rows and the parameters are under way while the chunks are joined
+        typename Vec<T, V>::type raw[U];
         float mean[V], mul[V], add[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = (cc + i) / a.cpg;
-            mean[i] = gmean[g];
-            mul[i] = grstd[g] * (a.gamma ? a.gamma[t.c0 + cc + i] : 1.0f);
-            add[i] = a.beta ? a.beta[t.c0 + cc + i] : 0.0f;
-        }
-        for (int row = t.row0 + rp; row < t.row1; row += U * t.rp) {
-            typename Vec<T, V>::type raw[U];
+        int row = t.row0 + rp;
+        const auto load = [&] {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                raw[u] = Vec<T, V>::load(x + (size_t)(row + u * t.rp < t.row1 ? row + u * t.rp : row) * a.c + cc);
+                if (row + u * t.rp < t.row1) raw[u] = Vec<T, V>::load(x + (size_t)(row + u * t.rp) * a.c + cc);
+        };
+        if (active) {
+            load();
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                mul[i] = a.gamma ? a.gamma[t.c0 + cc + i] : 1.0f;
+                add[i] = a.beta ? a.beta[t.c0 + cc + i] : 0.0f;
+            }
+        }
+        if (!joined) {
+            join_chunks(a, t, g0, ng, gmean, grstd);
+            __syncthreads();
+            joined = true;
+        }
+        if (!active) continue;
+        for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
+            mean[i] = gmean[g];
+            mul[i] *= grstd[g];
+        });
+        for (; row < t.row1; row += U * t.rp, load()) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (row + u * t.rp >= t.row1) break;
                 float f[V];
                 Vec<T, V>::get(raw[u], f);
 #pragma unroll
                 for (int i = 0; i < V; ++i) f[i] = activate<ACT>(fmaf(f[i] - mean[i], mul[i], add[i]));
-                if (row + u * t.rp < t.row1) Vec<T, V>::store(y + (size_t)(row + u * t.rp) * a.c + cc, f);
+                Vec<T, V>::store(y + (size_t)(row + u * t.rp) * a.c + cc, f);
             }
         }
     }
 }
 
 // What a lane of the backward pass needs of its channels.
-template <int V> struct Channels {
+template <int V, bool WHOLE> struct Channels {
     float mean[V], rstd[V], gamma[V], beta[V];
-    __device__ __forceinline__ void load(const NormArgs &a, const Tile &t, int cc)
+    __device__ __forceinline__ void load(const NormArgs &a, const Tile &t, int g0, int cc)
     {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = t.c0 + cc + i, g = c / a.cpg;
-            mean[i] = a.mean[(size_t)t.sample * a.groups + g];
-            rstd[i] = a.rstd[(size_t)t.sample * a.groups + g];
-            gamma[i] = a.gamma ? a.gamma[c] : 1.0f;
-            beta[i] = a.beta ? a.beta[c] : 0.0f;
-        }
+        const size_t at = (size_t)t.sample * a.groups + g0;
+        for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
+            if (!WHOLE || i == 0) {
+                mean[i] = a.mean[at + g];
+                rstd[i] = a.rstd[at + g];
+            } else {
+                mean[i] = mean[0];
+                rstd[i] = rstd[0];
+            }
+            gamma[i] = a.gamma ? a.gamma[t.c0 + cc + i] : 1.0f;
+            beta[i] = a.beta ? a.beta[t.c0 + cc + i] : 0.0f;
+        });
     }
 };
 
-template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) void group_norm_grad_sums_kernel(NormArgs a)
+template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_grad_sums_kernel(NormArgs a)
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
     float *lane1 = lds, *lane2 = lds + kThreads * V, *group = lds + 2 * kThreads * V;
     const Tile t = tile_of<V>(a, blockIdx.x);
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
-    const int col = threadIdx.x % t.cols, rp = threadIdx.x / t.cols;
+    int col;
+    const int rp = fast_div(threadIdx.x, t.cols, 1.0f / (float)t.cols, &col);
     const size_t at0 = ((size_t)t.sample * a.p) * a.c + t.c0;
     const T *x = static_cast<const T *>(a.x) + at0, *dy = static_cast<const T *>(a.dy) + at0;
     for (int g = threadIdx.x; g < ng; g += kThreads) group[2 * g] = group[2 * g + 1] = 0.0f;
@@ -339,16 +415,21 @@ template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) voi
 #pragma unroll
         for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.0f;
         if (rp < t.rp && cc < t.width) {
-            Channels<V> k;
-            k.load(a, t, cc);
-            for (int row = t.row0 + rp; row < t.row1; row += U * t.rp) {
-                typename Vec<T, V>::type rx[U], rd[U];
+            int row = t.row0 + rp;
+            typename Vec<T, V>::type rx[U], rd[U];
+            const auto load = [&] {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const size_t at = (size_t)(row + u * t.rp < t.row1 ? row + u * t.rp : row) * a.c + cc;
-                    rx[u] = Vec<T, V>::load(x + at);
-                    rd[u] = Vec<T, V>::load(dy + at);
-                }
+                for (int u = 0; u < U; ++u)
+                    if (row + u * t.rp < t.row1) {
+                        const size_t at = (size_t)(row + u * t.rp) * a.c + cc;
+                        rx[u] = Vec<T, V>::load(x + at);
+                        rd[u] = Vec<T, V>::load(dy + at);
+                    }
+            };
+            load();
+            Channels<V, WHOLE> k;
+            k.load(a, t, g0, cc);
+            for (; row < t.row1; row += U * t.rp, load()) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (row + u * t.rp >= t.row1) break;
@@ -375,6 +456,7 @@ template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) voi
         // per channel, into the first row of lanes and the workspace
         for (int c = threadIdx.x; c < pass_width; c += kThreads) {
             float v1 = 0.0f, v2 = 0.0f;
+#pragma unroll 8
             for (int r = 0; r < t.rp; ++r) {
                 v1 += lane1[r * t.cols * V + c];
                 v2 += lane2[r * t.cols * V + c];
@@ -414,15 +496,15 @@ template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) voi
 constexpr int kReduceChannels = 16;        // channels of a workgroup that adds up dgamma and dbeta
 
 // dgamma and dbeta of kReduceChannels channels: the sums of all samples' chunks.
-__device__ __forceinline__ void reduce_channels(const NormArgs &a, int c0, float *lds)
+__device__ __forceinline__ void reduce_channels(const NormArgs &a, const float *chan, int rows, int c0, float *lds)
 {
     const int lc = threadIdx.x % kReduceChannels, lr = threadIdx.x / kReduceChannels, c = c0 + lc;
     constexpr int kLanes = kThreads / kReduceChannels;
     float v1 = 0.0f, v2 = 0.0f;
     if (c < a.c)
 #pragma unroll 8
-        for (int r = lr; r < a.n * a.chunks; r += kLanes) {
-            const float2 v = reinterpret_cast<const float2 *>(a.chan)[(size_t)r * a.c + c];
+        for (int r = lr; r < rows; r += kLanes) {
+            const float2 v = reinterpret_cast<const float2 *>(chan)[(size_t)r * a.c + c];
             v1 += v.x;
             v2 += v.y;
         }
@@ -440,60 +522,74 @@ __device__ __forceinline__ void reduce_channels(const NormArgs &a, int c0, float
 }
 
 // The first workgroups add up dgamma and dbeta, the others write dx.
-template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers)
+template <typename T, int V, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers, const float *chan, int chan_rows)
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
     if ((int)blockIdx.x < reducers) {
-        reduce_channels(a, blockIdx.x * kReduceChannels, lds);
+        reduce_channels(a, chan, chan_rows, blockIdx.x * kReduceChannels, lds);
         return;
     }
     const Tile t = tile_of<V>(a, blockIdx.x - reducers);
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
     float *ga = lds, *gb = lds + ng;
-    {
-        const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
-        const float inv = 1.0f / ((float)a.p * (float)a.cpg);
-        for (int g = team; g < ng; g += kThreads / kTeam) {
-            const float *part = a.part + ((size_t)t.sample * a.groups + g0 + g) * a.chunks * 2;
-            float v1 = 0.0f, v2 = 0.0f;
-            for (int k = tl; k < a.chunks; k += kTeam) {
-                v1 += part[2 * k];
-                v2 += part[2 * k + 1];
-            }
-            v1 = team_sum(v1);
-            v2 = team_sum(v2);
-            if (tl == 0) {
-                ga[g] = v1 * inv;
-                gb[g] = v2 * inv;
-            }
-        }
-    }
-    __syncthreads();
-    const int col = threadIdx.x % t.cols, rp = threadIdx.x / t.cols;
-    if (rp >= t.rp) return;
+    int col;
+    const int rp = fast_div(threadIdx.x, t.cols, 1.0f / (float)t.cols, &col);
     const size_t at0 = ((size_t)t.sample * a.p) * a.c + t.c0;
     const T *x = static_cast<const T *>(a.x) + at0, *dy = static_cast<const T *>(a.dy) + at0;
     T *dx = static_cast<T *>(a.y) + at0;
-    for (int cc = col * V; cc < t.width; cc += t.cols * V) {
-        Channels<V> k;
-        k.load(a, t, cc);
-        float sa[V], sb[V];
+    bool joined = false;
+    for (int cc = col * V, pass = 0; pass * t.cols * V < t.width; ++pass, cc += t.cols * V) {
+        const bool active = rp < t.rp && cc < t.width;
+        typename Vec<T, V>::type rx[U], rd[U];
+        int row = t.row0 + rp;
+        const auto load = [&] {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            sa[i] = ga[(cc + i) / a.cpg];
-            sb[i] = gb[(cc + i) / a.cpg];
+            for (int u = 0; u < U; ++u)
+                if (row + u * t.rp < t.row1) {
+                    const size_t at = (size_t)(row + u * t.rp) * a.c + cc;
+                    rx[u] = Vec<T, V>::load(x + at);
+                    rd[u] = Vec<T, V>::load(dy + at);
+                }
+        };
+        Channels<V, WHOLE> k;
+        if (active) {
+            load();
+            k.load(a, t, g0, cc);
         }
-        for (int row = t.row0 + rp; row < t.row1; row += U * t.rp) {
-            typename Vec<T, V>::type rx[U], rd[U];
+        if (!joined) {
+            const int team = threadIdx.x / kPairTeam, tl = threadIdx.x % kPairTeam;
+            const float inv = 1.0f / ((float)a.p * (float)a.cpg);
+            for (int g = team; g < ng; g += kThreads / kPairTeam) {
+                float2 v[kPairs];
+                load_pairs(a, t.sample, g0 + g, tl, v);
+                float v1 = 0.0f, v2 = 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t at = (size_t)(row + u * t.rp < t.row1 ? row + u * t.rp : row) * a.c + cc;
-                rx[u] = Vec<T, V>::load(x + at);
-                rd[u] = Vec<T, V>::load(dy + at);
+                for (int i = 0; i < kPairs; ++i) {
+                    v1 += v[i].x;
+                    v2 += v[i].y;
+                }
+                v1 = team_sum<kPairTeam>(v1);
+                v2 = team_sum<kPairTeam>(v2);
+                if (tl == 0) {
+                    ga[g] = v1 * inv;
+                    gb[g] = v2 * inv;
+                }
             }
+            __syncthreads();
+            joined = true;
+        }
+        if (!active) continue;
+        float sa[V], sb[V];
+        for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
+            sa[i] = ga[g];
+            sb[i] = gb[g];
+        });
+        for (; row < t.row1; row += U * t.rp, load()) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (row + u * t.rp >= t.row1) break;
                 float fx[V], fd[V];
                 Vec<T, V>::get(rx[u], fx);
                 Vec<T, V>::get(rd[u], fd);
@@ -503,35 +599,209 @@ template <typename T, int V, int ACT> __global__ __launch_bounds__(kThreads) voi
                     const float dz = activate_grad<ACT>(fd[i], fmaf(xhat, k.gamma[i], k.beta[i]));
                     fx[i] = k.rstd[i] * (fmaf(k.gamma[i], dz, -sa[i]) - xhat * sb[i]);
                 }
-                if (row + u * t.rp < t.row1) Vec<T, V>::store(dx + (size_t)(row + u * t.rp) * a.c + cc, fx);
+                Vec<T, V>::store(dx + (size_t)(row + u * t.rp) * a.c + cc, fx);
             }
         }
     }
 }
 
-template <typename T, int V> tvg_status launch_forward(const NormArgs &a, int act, const NormPlan &plan, hipStream_t stream)
+// ---------------------------------------------------------------------------------------
+// One launch, where a sample's block of channels fits the registers of a workgroup: NV vectors a lane, read once.
+// Mean first, then the squared distances from it, both over the workgroup's LDS.
+// ---------------------------------------------------------------------------------------
+
+// Sums over the channels and lanes of every group, given a value per channel and lane in LDS ([rp][width]); f(group, sum) by
+// one lane of the group's team.
+template <typename F>
+__device__ __forceinline__ void sum_groups(const float *values, int width, int rp, int cpg, int ng, int team, int threads, F &&f)
 {
-    const dim3 grid(a.tiles), threads(kThreads);
-    hipLaunchKernelGGL((group_norm_stats_kernel<T, V>), grid, threads, plan.lds_stats, stream, a);
-    if (act == TVG_ACT_SILU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_SILU>), grid, threads, plan.lds_apply, stream, a);
-    else if (act == TVG_ACT_RELU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_RELU>), grid, threads, plan.lds_apply, stream, a);
-    else hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_NONE>), grid, threads, plan.lds_apply, stream, a);
+    const int tl = threadIdx.x & (team - 1);
+    const float inv = 1.0f / (float)cpg;
+    for (int g = threadIdx.x / team; g < ng; g += threads / team) {
+        float s = 0.0f;
+        for (int e = tl; e < rp * cpg; e += team) {
+            int c;
+            const int r = fast_div(e, cpg, inv, &c);
+            s += values[r * width + g * cpg + c];
+        }
+        for (int d = 1; d < team; d *= 2) s += __shfl_xor(s, d);
+        if (tl == 0) f(g, s);
+    }
+}
+
+template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launch_bounds__(THREADS) void group_norm_once_kernel(NormArgs a, int team)
+{
+    constexpr int Q = WHOLE ? 1 : V;                       // entries per lane
+    extern __shared__ float lds[];
+    const int b = xcd_remap(blockIdx.x, a.tiles);          // (neighbouring blocks share lines of memory)
+    const int sample = b / a.blocks, c0 = (b - sample * a.blocks) * a.block, width = min(a.block, a.c - c0);
+    const int cols = width / V, ng = width / a.cpg;
+    int col;
+    const int rp = THREADS / cols, lane_row = fast_div(threadIdx.x, cols, 1.0f / (float)cols, &col);
+    const bool active = lane_row < rp;
+    const int cc = col * V;
+    float *values = lds, *gmean = lds + THREADS * Q, *grstd = gmean + ng;
+    const size_t at0 = ((size_t)sample * a.p) * a.c + c0 + cc;
+    const T *x = static_cast<const T *>(a.x) + at0;
+    T *y = static_cast<T *>(a.y) + at0;
+    typename Vec<T, V>::type raw[NV];
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        const int row = lane_row + u * rp;
+        if (active && row < a.p) raw[u] = Vec<T, V>::load(x + (size_t)row * a.c);
+    }
+    float mul[V], add[V], sum[V], mean[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        mul[i] = a.gamma ? a.gamma[c0 + cc + i] : 1.0f;
+        add[i] = a.beta ? a.beta[c0 + cc + i] : 0.0f;
+        sum[i] = 0.0f;
+    }
+    const auto put = [&] {                                 // the lane's sums to LDS
+        if (!active) return;
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int d = 1; d < V; d *= 2)
+#pragma unroll
+                for (int i = 0; i < V; i += 2 * d) sum[i] += sum[i + d];
+            values[lane_row * cols + col] = sum[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) values[lane_row * width + cc + i] = sum[i];
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+        if (active && lane_row + u * rp < a.p) {
+            float f[V];
+            Vec<T, V>::get(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += f[i];
+        }
+    put();
+    __syncthreads();
+    const float count = (float)a.p * (float)a.cpg;
+    constexpr int P = V / Q;                               // channels per entry
+    sum_groups(values, width / P, rp, a.cpg / P, ng, team, THREADS, [&](int g, float s) { gmean[g] = s / count; });
+    __syncthreads();
+    if (active) for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) { mean[i] = gmean[g]; });
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+        if (active && lane_row + u * rp < a.p) {
+            float f[V];
+            Vec<T, V>::get(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = f[i] - mean[i];
+                sum[i] = fmaf(d, d, sum[i]);
+            }
+        }
+    put();
+    __syncthreads();
+    const size_t stat = (size_t)sample * a.groups + c0 / a.cpg;
+    sum_groups(values, width / P, rp, a.cpg / P, ng, team, THREADS, [&](int g, float s) {
+        const float r = 1.0f / sqrtf(s / count + a.eps);
+        grstd[g] = r;
+        if (a.mean) a.mean[stat + g] = gmean[g];
+        if (a.rstd) a.rstd[stat + g] = r;
+    });
+    __syncthreads();
+    if (!active) return;
+    for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) { mul[i] *= grstd[g]; });
+    const auto write = [&](auto act) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int row = lane_row + u * rp;
+            if (row >= a.p) break;
+            float f[V];
+            Vec<T, V>::get(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = activate<decltype(act)::value>(fmaf(f[i] - mean[i], mul[i], add[i]));
+            Vec<T, V>::store(y + (size_t)row * a.c, f);
+        }
+    };
+    if (a.act == TVG_ACT_SILU) write(std::integral_constant<int, TVG_ACT_SILU>());
+    else if (a.act == TVG_ACT_RELU) write(std::integral_constant<int, TVG_ACT_RELU>());
+    else write(std::integral_constant<int, TVG_ACT_NONE>());
+}
+
+template <typename T, int V, bool WHOLE> tvg_status launch_once(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    const int ng = a.block / a.cpg;
+    int team = 64;
+    while (team > 1 && ng * team > plan.threads) team /= 2;
+    const size_t lds = ((size_t)plan.threads * V + 2 * ng) * sizeof(float);
+    if (plan.threads == 256) hipLaunchKernelGGL((group_norm_once_kernel<T, V, 4, 256, WHOLE>), dim3(a.tiles), dim3(256), lds, stream, a, team);
+    else if (plan.threads == 512) hipLaunchKernelGGL((group_norm_once_kernel<T, V, 8, 512, WHOLE>), dim3(a.tiles), dim3(512), lds, stream, a, team);
+    else hipLaunchKernelGGL((group_norm_once_kernel<T, V, 16, 1024, WHOLE>), dim3(a.tiles), dim3(1024), lds, stream, a, team);
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
-template <typename T, int V, int ACT> void launch_grad(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+// Whether a lane's channels are always of one group.
+template <int V> bool whole_vectors(const NormArgs &a) { return a.cpg % V == 0; }
+
+// The arguments of samples n0 to n0 + n.
+NormArgs samples(const NormArgs &a, int n0, int n, size_t elem)
 {
-    const int reducers = a.dgamma || a.dbeta ? (a.c + kReduceChannels - 1) / kReduceChannels : 0;
-    hipLaunchKernelGGL((group_norm_grad_sums_kernel<T, V, ACT>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
-    hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a, reducers);
+    NormArgs b = a;
+    const size_t at = (size_t)n0 * a.p * a.c * elem;
+    b.x = static_cast<const char *>(a.x) + at;
+    b.y = static_cast<char *>(a.y) + at;
+    if (a.dy) b.dy = static_cast<const char *>(a.dy) + at;
+    if (a.mean) b.mean += (size_t)n0 * a.groups;
+    if (a.rstd) b.rstd += (size_t)n0 * a.groups;
+    b.part += (size_t)n0 * a.groups * a.chunks * 2;
+    if (a.chan) b.chan += (size_t)n0 * a.chunks * a.c * 2;
+    b.n = n;
+    b.tiles = n * a.blocks * a.chunks;
+    return b;
 }
 
-template <typename T, int V> tvg_status launch_backward(const NormArgs &a, int act, const NormPlan &plan, hipStream_t stream)
+template <typename T, int V, bool WHOLE> tvg_status launch_forward(const NormArgs &all, const NormPlan &plan, hipStream_t stream)
 {
-    if (act == TVG_ACT_SILU) launch_grad<T, V, TVG_ACT_SILU>(a, plan, stream);
-    else if (act == TVG_ACT_RELU) launch_grad<T, V, TVG_ACT_RELU>(a, plan, stream);
-    else launch_grad<T, V, TVG_ACT_NONE>(a, plan, stream);
-    return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
+    if (plan.once) return launch_once<T, V, WHOLE>(all, plan, stream);
+    for (int n0 = 0; n0 < all.n; n0 += plan.batch) {
+        const NormArgs a = samples(all, n0, std::min(plan.batch, all.n - n0), sizeof(T));
+        const dim3 grid(a.tiles), threads(kThreads);
+        hipLaunchKernelGGL((group_norm_stats_kernel<T, V, WHOLE>), grid, threads, plan.lds_stats, stream, a);
+        if (a.act == TVG_ACT_SILU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_SILU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+        else if (a.act == TVG_ACT_RELU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_RELU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+        else hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_NONE, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+        if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
+    }
+    return TVG_OK;
+}
+template <typename T, int V> tvg_status launch_forward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    return whole_vectors<V>(a) ? launch_forward<T, V, true>(a, plan, stream) : launch_forward<T, V, false>(a, plan, stream);
+}
+
+template <typename T, int V, int ACT, bool WHOLE> tvg_status launch_grad(const NormArgs &all, const NormPlan &plan, hipStream_t stream)
+{
+    for (int n0 = 0; n0 < all.n; n0 += plan.batch) {
+        const NormArgs a = samples(all, n0, std::min(plan.batch, all.n - n0), sizeof(T));
+        // (the last launch has the sums of all samples)
+        const bool last = n0 + plan.batch >= all.n;
+        const int reducers = last && (a.dgamma || a.dbeta) ? (a.c + kReduceChannels - 1) / kReduceChannels : 0;
+        hipLaunchKernelGGL((group_norm_grad_sums_kernel<T, V, ACT, WHOLE>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
+        hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a,
+                           reducers, all.chan, all.n * all.chunks);
+        if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
+    }
+    return TVG_OK;
+}
+
+template <typename T, int V, bool WHOLE> tvg_status launch_backward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    if (a.act == TVG_ACT_SILU) return launch_grad<T, V, TVG_ACT_SILU, WHOLE>(a, plan, stream);
+    if (a.act == TVG_ACT_RELU) return launch_grad<T, V, TVG_ACT_RELU, WHOLE>(a, plan, stream);
+    return launch_grad<T, V, TVG_ACT_NONE, WHOLE>(a, plan, stream);
+}
+template <typename T, int V> tvg_status launch_backward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    return whole_vectors<V>(a) ? launch_backward<T, V, true>(a, plan, stream) : launch_backward<T, V, false>(a, plan, stream);
 }
 
 int gcd(int a, int b)
@@ -562,16 +832,52 @@ NormArgs make_args(const NormProblem &p, const NormPlan &plan)
     a.block = plan.block; a.blocks = plan.blocks; a.rows = plan.rows; a.chunks = plan.chunks;
     a.tiles = p.n * plan.blocks * plan.chunks;
     a.eps = p.eps;
+    a.act = p.act;
     return a;
 }
 
 }  // namespace
 
+// The plan of one launch, if a block of channels fits a workgroup's registers: blocks for a workgroup a CU, 64 bytes of a row
+// at least where that fits, 32 at least.
+static bool plan_once(const NormProblem &p, int vector, NormPlan *plan)
+{
+    const int cpg = p.c / p.groups, size = p.dtype == TVG_BF16 ? 2 : 4;
+    const int unit = cpg / gcd(cpg, vector) * vector;                  // divides c: so do both
+    static const int kLanes[3] = {256, 512, 1024}, kVectors[3] = {4, 8, 16};
+    const auto fits = [&](int width, int k) {
+        const int cols = width / vector;
+        return cols <= kLanes[k] && width / cpg <= 2048 && ((int64_t)p.p + kLanes[k] / cols - 1) / (kLanes[k] / cols) <= kVectors[k];
+    };
+    int64_t units = std::max<int64_t>((int64_t)p.n * p.c / kComputeUnits / unit, (64 / size + unit - 1) / unit);
+    units = std::min<int64_t>(units, p.c / unit);
+    while (units > 1 && !fits((int)units * unit, 2)) --units;
+    const int width = (int)units * unit;
+    // (few workgroups with much each: the two launches spread it)
+    if ((int64_t)p.n * ((p.c + width - 1) / width) < kComputeUnits / 2 && (int64_t)p.p * width * size > 32 * 1024) return false;
+    if (!fits(width, 2) || (width * size < 32 && width < p.c)) return false;
+    int k = 0;
+    while (!fits(width, k)) ++k;
+    plan->once = true;
+    plan->threads = kLanes[k];
+    plan->block = width;
+    plan->blocks = (p.c + width - 1) / width;
+    plan->rows = p.p;
+    plan->chunks = 1;
+    plan->part_floats = plan->chan_floats = 0;
+    return true;
+}
+
+constexpr int64_t kBatchBytes = (int64_t)100 << 40;
+
 // Row chunks: as many workgroups as keep every CU busy, with eight vectors a lane at least and 64 chunks of a sample at
 // most, whose statistics every workgroup of the second launch joins.
-void plan_group_norm(const NormProblem &p, int vector, NormPlan *plan)
+static void plan_group_norm(const NormProblem &p, int vector, bool backward, NormPlan *plan)
 {
     const int cpg = p.c / p.groups;
+    plan->once = false;
+    plan->vector = vector;
+    if (!backward && plan_once(p, vector, plan)) return;
     // a block of whole groups and whole vectors, as wide as one pass of the workgroup
     const int64_t unit = (int64_t)cpg * vector / gcd(cpg, vector);
     const int64_t most = (int64_t)kThreads * vector;
@@ -579,7 +885,12 @@ void plan_group_norm(const NormProblem &p, int vector, NormPlan *plan)
     plan->block = unit >= p.c ? p.c : p.c <= most ? p.c : (int)(unit * std::max<int64_t>(1, most / unit));
     plan->blocks = (p.c + plan->block - 1) / plan->block;
     const int cols = std::min(plan->block / vector, kThreads), rp = kThreads / cols;
-    const int64_t want = std::max<int64_t>(1, 8 * kComputeUnits / ((int64_t)p.n * plan->blocks));
+    // Samples at a time: what the first launch reads is in the memory-side cache (256 MB) when the second reads it again.
+    const int64_t sample = (int64_t)p.p * p.c * (p.dtype == TVG_BF16 ? 2 : 4) * (backward ? 2 : 1);
+    const int most_at_once = (int)std::min<int64_t>(p.n, std::max<int64_t>(1, kBatchBytes / sample));
+    const int batches = (p.n + most_at_once - 1) / most_at_once;
+    plan->batch = (p.n + batches - 1) / batches;
+    const int64_t want = std::max<int64_t>(1, 8 * kComputeUnits / ((int64_t)plan->batch * plan->blocks));
     int64_t chunks = std::min<int64_t>(std::min<int64_t>(want, 64), std::max<int64_t>(1, p.p / (8 * rp)));
     plan->rows = (int)((p.p + chunks - 1) / chunks);
     plan->chunks = (p.p + plan->rows - 1) / plan->rows;
@@ -591,40 +902,38 @@ void plan_group_norm(const NormProblem &p, int vector, NormPlan *plan)
 }
 
 // The workspace holds what any alignment of the tensors needs.
-static NormPlan widest_plan(const NormProblem &p, bool backward, size_t *bytes)
+static size_t largest_workspace(const NormProblem &p, bool backward)
 {
+    size_t bytes = 0;
     NormPlan plan;
-    *bytes = 0;
     for (int v = vector_width(p, {}); v >= 1; v /= 2) {
-        plan_group_norm(p, v, &plan);
-        *bytes = std::max(*bytes, (plan.part_floats + (backward ? plan.chan_floats : 0)) * sizeof(float));
+        plan_group_norm(p, v, backward, &plan);
+        bytes = std::max(bytes, (plan.part_floats + (backward ? plan.chan_floats : 0)) * sizeof(float));
     }
-    return plan;
+    return bytes;
 }
 
 size_t group_norm_workspace(const NormProblem &p, bool backward)
 {
-    size_t bytes;
-    widest_plan(p, backward, &bytes);
-    return bytes;
+    return largest_workspace(p, backward);
 }
 
 tvg_status launch_group_norm(const NormProblem &p, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                              float *rstd, float *workspace, hipStream_t stream)
 {
     NormPlan plan;
-    plan_group_norm(p, vector_width(p, {x, y}), &plan);
+    plan_group_norm(p, vector_width(p, {x, y}), false, &plan);
     NormArgs a = make_args(p, plan);
     a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.mean = mean; a.rstd = rstd; a.part = workspace;
     if (p.dtype == TVG_BF16) {
-        if (plan.vector == 8) return launch_forward<bf16_t, 8>(a, p.act, plan, stream);
-        if (plan.vector == 4) return launch_forward<bf16_t, 4>(a, p.act, plan, stream);
-        if (plan.vector == 2) return launch_forward<bf16_t, 2>(a, p.act, plan, stream);
-        return launch_forward<bf16_t, 1>(a, p.act, plan, stream);
+        if (plan.vector == 8) return launch_forward<bf16_t, 8>(a, plan, stream);
+        if (plan.vector == 4) return launch_forward<bf16_t, 4>(a, plan, stream);
+        if (plan.vector == 2) return launch_forward<bf16_t, 2>(a, plan, stream);
+        return launch_forward<bf16_t, 1>(a, plan, stream);
     }
-    if (plan.vector == 4) return launch_forward<float, 4>(a, p.act, plan, stream);
-    if (plan.vector == 2) return launch_forward<float, 2>(a, p.act, plan, stream);
-    return launch_forward<float, 1>(a, p.act, plan, stream);
+    if (plan.vector == 4) return launch_forward<float, 4>(a, plan, stream);
+    if (plan.vector == 2) return launch_forward<float, 2>(a, plan, stream);
+    return launch_forward<float, 1>(a, plan, stream);
 }
 
 tvg_status launch_group_norm_backward(const NormProblem &p, const void *x, const void *dy, const float *mean, const float *rstd,
@@ -632,21 +941,21 @@ tvg_status launch_group_norm_backward(const NormProblem &p, const void *x, const
                                       float *workspace, hipStream_t stream)
 {
     NormPlan plan;
-    plan_group_norm(p, vector_width(p, {x, dy, dx}), &plan);
+    plan_group_norm(p, vector_width(p, {x, dy, dx}), true, &plan);
     NormArgs a = make_args(p, plan);
     a.x = x; a.dy = dy; a.gamma = gamma; a.beta = beta; a.y = dx; a.dgamma = dgamma; a.dbeta = dbeta;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.chan = workspace;                    // (first: read as pairs)
     a.part = workspace + plan.chan_floats;
     if (p.dtype == TVG_BF16) {
-        if (plan.vector == 8) return launch_backward<bf16_t, 8>(a, p.act, plan, stream);
-        if (plan.vector == 4) return launch_backward<bf16_t, 4>(a, p.act, plan, stream);
-        if (plan.vector == 2) return launch_backward<bf16_t, 2>(a, p.act, plan, stream);
-        return launch_backward<bf16_t, 1>(a, p.act, plan, stream);
+        if (plan.vector == 8) return launch_backward<bf16_t, 8>(a, plan, stream);
+        if (plan.vector == 4) return launch_backward<bf16_t, 4>(a, plan, stream);
+        if (plan.vector == 2) return launch_backward<bf16_t, 2>(a, plan, stream);
+        return launch_backward<bf16_t, 1>(a, plan, stream);
     }
-    if (plan.vector == 4) return launch_backward<float, 4>(a, p.act, plan, stream);
-    if (plan.vector == 2) return launch_backward<float, 2>(a, p.act, plan, stream);
-    return launch_backward<float, 1>(a, p.act, plan, stream);
+    if (plan.vector == 4) return launch_backward<float, 4>(a, plan, stream);
+    if (plan.vector == 2) return launch_backward<float, 2>(a, plan, stream);
+    return launch_backward<float, 1>(a, plan, stream);
 }
 
 }  // namespace tvg

@@ -272,12 +272,14 @@ struct NormProblem {
 };
 struct NormPlan {
     int vector;                       // channels per lane
+    bool once;                        // one launch, of `threads` lanes a workgroup
+    int threads;
+    int batch;                        // samples per pair of launches
     int block, blocks;                // channels per workgroup, workgroups across the channels
     int rows, chunks;                 // rows per workgroup, workgroups across the rows
     size_t lds_stats, lds_apply;
     size_t part_floats, chan_floats;  // workspace: per group and chunk, per channel and chunk
 };
-void plan_group_norm(const NormProblem &p, int vector, NormPlan *plan);
 size_t group_norm_workspace(const NormProblem &p, bool backward);
 tvg_status launch_group_norm(const NormProblem &p, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                              float *rstd, float *workspace, hipStream_t stream);

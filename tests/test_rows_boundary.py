@@ -70,7 +70,7 @@ def test_pointers_workspaces_and_alignment():
         assert tvg.tvg_group_norm_fused_backward(d, *args, p, back, 0) == 1
     for ws, size in ((0, back), (p + 128, back), (p, back - 1)):
         assert tvg.tvg_group_norm_fused_backward(d, *[p] * 9, ws, size, 0) == 4
-    d = norm(n=64, pixels=3136, c=256, groups=32)              # (a map that one launch cannot take)
+    d = norm(n=64, pixels=12544, c=256, groups=32)             # (a map that one launch cannot take)
     need = tvg.tvg_group_norm_workspace_size(d)
     assert need > 0
     for ws, size in ((0, need), (p + 128, need), (p, need - 1)):
