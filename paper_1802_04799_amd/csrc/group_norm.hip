@@ -7,7 +7,8 @@
 //   with a, b the sums of gamma S1, gamma S2 over a group's channels and m its elements
 //
 // Bound by memory: about 10 (forward) or 25 (backward) operations an element.  Two launches: the first leaves partial
-// statistics of row chunks in the workspace, the second joins those of its sample in a fixed order and applies them.
+// statistics of row chunks in the workspace, the second joins those of its sample in a fixed order and applies them, the last
+// chunk first: it is the one whose rows the caches still hold.
 //
 // A workgroup covers a chunk of rows of one sample and a block of whole groups; a lane covers V adjacent channels (16
 // bytes where the channels allow it) of every RP-th row, so that what it needs of a channel stays in registers and groups
@@ -65,20 +66,20 @@ template <typename T> struct Vec<T, 1> {
     static __device__ __forceinline__ void store(T *p, const float *f) { Elem<T>::store(p, 0, f[0]); }
 };
 
-template <int ACT> __device__ __forceinline__ float activate(float z)
+template <typename T, int ACT> __device__ __forceinline__ float activate(float z)
 {
     if constexpr (ACT == TVG_ACT_RELU) return z < 0.0f ? 0.0f : z;      // (a NaN stays one)
-    if constexpr (ACT == TVG_ACT_SILU) return z * sigmoid(z);
+    if constexpr (ACT == TVG_ACT_SILU) return z * sigmoid<sizeof(T) == 4>(z);
     return z;
 }
 
 // dy times the activation's derivative at z
-template <int ACT> __device__ __forceinline__ float activate_grad(float dy, float z)
+template <typename T, int ACT> __device__ __forceinline__ float activate_grad(float dy, float z)
 {
     if constexpr (ACT == TVG_ACT_RELU) return z <= 0.0f ? 0.0f : dy;
     if constexpr (ACT == TVG_ACT_SILU) {
-        const float s = sigmoid(z);
-        return dy * (s * fmaf(z, 1.0f - s, 1.0f));
+        const float s = sigmoid<sizeof(T) == 4>(z), t = z * s;         // s (1 + z (1 - s))
+        return dy * fmaf(-t, s, s + t);
     }
     return dy;
 }
@@ -141,14 +142,14 @@ template <int V, bool WHOLE, typename F> __device__ __forceinline__ void for_cha
     }
 }
 
-// The pairs of a group's chunks, eight lanes a group: all loads of a lane are under way together.
-constexpr int kPairTeam = 8, kPairs = 64 / kPairTeam;
-__device__ __forceinline__ void load_pairs(const NormArgs &a, int sample, int group, int tl, float2 (&v)[kPairs])
+// The pairs of a group's chunks k0 to k0 + 63, eight lanes a group: all loads of a lane are under way together.
+constexpr int kPairTeam = 8, kPairs = 8, kPairChunks = kPairTeam * kPairs;
+__device__ __forceinline__ void load_pairs(const NormArgs &a, int sample, int group, int k0, int tl, float2 (&v)[kPairs])
 {
     const float2 *part = reinterpret_cast<const float2 *>(a.part) + ((size_t)sample * a.groups + group) * a.chunks;
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-        const int k = tl + i * kPairTeam;
+        const int k = k0 + tl + i * kPairTeam;
         v[i] = k < a.chunks ? part[k] : float2{0.0f, 0.0f};
     }
 }
@@ -299,16 +300,21 @@ __device__ __forceinline__ void join_chunks(const NormArgs &a, const Tile &t, in
     const float total = (float)a.p;                        // (in rows: every chunk has cpg channels a row)
     for (int g = team; g < ng; g += kThreads / kPairTeam) {
         float2 v[kPairs];
-        load_pairs(a, t.sample, g0 + g, tl, v);
-        float s = 0.0f;
+        const auto rows = [&](int k) { return (float)max(0, min(a.rows, a.p - k * a.rows)); };
+        float s = 0.0f, q = 0.0f;
+        for (int k0 = 0; k0 < a.chunks; k0 += kPairChunks) {
+            load_pairs(a, t.sample, g0 + g, k0, tl, v);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) s += (float)max(0, min(a.rows, a.p - (tl + i * kPairTeam) * a.rows)) * v[i].x;
+            for (int i = 0; i < kPairs; ++i) s += rows(k0 + tl + i * kPairTeam) * v[i].x;
+        }
         const float m = team_sum<kPairTeam>(s) / total;
-        float q = 0.0f;
+        for (int k0 = 0; k0 < a.chunks; k0 += kPairChunks) {
+            if (a.chunks > kPairChunks) load_pairs(a, t.sample, g0 + g, k0, tl, v);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-            const float d = v[i].x - m, n = (float)max(0, min(a.rows, a.p - (tl + i * kPairTeam) * a.rows)) * (float)a.cpg;
-            q += n > 0.0f ? fmaf(d * d, n, v[i].y) : 0.0f;
+            for (int i = 0; i < kPairs; ++i) {
+                const float d = v[i].x - m, n = rows(k0 + tl + i * kPairTeam) * (float)a.cpg;
+                q += n > 0.0f ? fmaf(d * d, n, v[i].y) : 0.0f;
+            }
         }
         q = team_sum<kPairTeam>(q);
         if (tl == 0) {
@@ -325,7 +331,7 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
-    const Tile t = tile_of<V>(a, blockIdx.x);
+    const Tile t = tile_of<V>(a, a.tiles - 1 - blockIdx.x);
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
     float *gmean = lds, *grstd = lds + ng;
     int col;
@@ -369,16 +375,17 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
                 float f[V];
                 Vec<T, V>::get(raw[u], f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = activate<ACT>(fmaf(f[i] - mean[i], mul[i], add[i]));
+                for (int i = 0; i < V; ++i) f[i] = activate<T, ACT>(fmaf(f[i] - mean[i], mul[i], add[i]));
                 Vec<T, V>::store(y + (size_t)(row + u * t.rp) * a.c + cc, f);
             }
         }
     }
 }
 
-// What a lane of the backward pass needs of its channels.
+// What a lane of the backward pass needs of its channels: with d = x - mean, z = mul d + add, S2 = rstd sum dz d, and
+// dx = mul dz - (rstd a + rstd^2 b d).
 template <int V, bool WHOLE> struct Channels {
-    float mean[V], rstd[V], gamma[V], beta[V];
+    float mean[V], rstd[V], mul[V], add[V];
     __device__ __forceinline__ void load(const NormArgs &a, const Tile &t, int g0, int cc)
     {
         const size_t at = (size_t)t.sample * a.groups + g0;
@@ -390,9 +397,11 @@ template <int V, bool WHOLE> struct Channels {
                 mean[i] = mean[0];
                 rstd[i] = rstd[0];
             }
-            gamma[i] = a.gamma ? a.gamma[t.c0 + cc + i] : 1.0f;
-            beta[i] = a.beta ? a.beta[t.c0 + cc + i] : 0.0f;
+            mul[i] = a.gamma ? a.gamma[t.c0 + cc + i] : 1.0f;
+            add[i] = a.beta ? a.beta[t.c0 + cc + i] : 0.0f;
         });
+#pragma unroll
+        for (int i = 0; i < V; ++i) mul[i] *= rstd[i];
     }
 };
 
@@ -438,13 +447,15 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
                     Vec<T, V>::get(rd[u], fd);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float xhat = (fx[i] - k.mean[i]) * k.rstd[i];
-                        const float dz = activate_grad<ACT>(fd[i], fmaf(xhat, k.gamma[i], k.beta[i]));
+                        const float d = fx[i] - k.mean[i];
+                        const float dz = activate_grad<T, ACT>(fd[i], fmaf(d, k.mul[i], k.add[i]));
                         s1[i] += dz;
-                        s2[i] = fmaf(dz, xhat, s2[i]);
+                        s2[i] = fmaf(dz, d, s2[i]);
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < V; ++i) s2[i] *= k.rstd[i];
         }
         __syncthreads();
 #pragma unroll
@@ -496,7 +507,7 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
 constexpr int kReduceChannels = 16;        // channels of a workgroup that adds up dgamma and dbeta
 
 // dgamma and dbeta of kReduceChannels channels: the sums of all samples' chunks.
-__device__ __forceinline__ void reduce_channels(const NormArgs &a, const float *chan, int rows, int c0, float *lds)
+__device__ __forceinline__ void reduce_channels(const NormArgs &a, int rows, int c0, float *lds)
 {
     const int lc = threadIdx.x % kReduceChannels, lr = threadIdx.x / kReduceChannels, c = c0 + lc;
     constexpr int kLanes = kThreads / kReduceChannels;
@@ -504,7 +515,7 @@ __device__ __forceinline__ void reduce_channels(const NormArgs &a, const float *
     if (c < a.c)
 #pragma unroll 8
         for (int r = lr; r < rows; r += kLanes) {
-            const float2 v = reinterpret_cast<const float2 *>(chan)[(size_t)r * a.c + c];
+            const float2 v = reinterpret_cast<const float2 *>(a.chan)[(size_t)r * a.c + c];
             v1 += v.x;
             v2 += v.y;
         }
@@ -523,15 +534,15 @@ __device__ __forceinline__ void reduce_channels(const NormArgs &a, const float *
 
 // The first workgroups add up dgamma and dbeta, the others write dx.
 template <typename T, int V, int ACT, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers, const float *chan, int chan_rows)
+__global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers)
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
     if ((int)blockIdx.x < reducers) {
-        reduce_channels(a, chan, chan_rows, blockIdx.x * kReduceChannels, lds);
+        reduce_channels(a, a.n * a.chunks, blockIdx.x * kReduceChannels, lds);
         return;
     }
-    const Tile t = tile_of<V>(a, blockIdx.x - reducers);
+    const Tile t = tile_of<V>(a, a.tiles - 1 - (blockIdx.x - reducers));
     const int g0 = t.c0 / a.cpg, ng = t.width / a.cpg;
     float *ga = lds, *gb = lds + ng;
     int col;
@@ -562,13 +573,15 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
             const int team = threadIdx.x / kPairTeam, tl = threadIdx.x % kPairTeam;
             const float inv = 1.0f / ((float)a.p * (float)a.cpg);
             for (int g = team; g < ng; g += kThreads / kPairTeam) {
-                float2 v[kPairs];
-                load_pairs(a, t.sample, g0 + g, tl, v);
                 float v1 = 0.0f, v2 = 0.0f;
+                for (int k0 = 0; k0 < a.chunks; k0 += kPairChunks) {
+                    float2 v[kPairs];
+                    load_pairs(a, t.sample, g0 + g, k0, tl, v);
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    v1 += v[i].x;
-                    v2 += v[i].y;
+                    for (int i = 0; i < kPairs; ++i) {
+                        v1 += v[i].x;
+                        v2 += v[i].y;
+                    }
                 }
                 v1 = team_sum<kPairTeam>(v1);
                 v2 = team_sum<kPairTeam>(v2);
@@ -583,8 +596,8 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
         if (!active) continue;
         float sa[V], sb[V];
         for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
-            sa[i] = ga[g];
-            sb[i] = gb[g];
+            sa[i] = ga[g] * k.rstd[i];
+            sb[i] = gb[g] * (k.rstd[i] * k.rstd[i]);
         });
         for (; row < t.row1; row += U * t.rp, load()) {
 #pragma unroll
@@ -595,9 +608,9 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
                 Vec<T, V>::get(rd[u], fd);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float xhat = (fx[i] - k.mean[i]) * k.rstd[i];
-                    const float dz = activate_grad<ACT>(fd[i], fmaf(xhat, k.gamma[i], k.beta[i]));
-                    fx[i] = k.rstd[i] * (fmaf(k.gamma[i], dz, -sa[i]) - xhat * sb[i]);
+                    const float d = fx[i] - k.mean[i];
+                    const float dz = activate_grad<T, ACT>(fd[i], fmaf(d, k.mul[i], k.add[i]));
+                    fx[i] = fmaf(dz, k.mul[i], -fmaf(d, sb[i], sa[i]));
                 }
                 Vec<T, V>::store(dx + (size_t)(row + u * t.rp) * a.c + cc, fx);
             }
@@ -718,7 +731,7 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
             float f[V];
             Vec<T, V>::get(raw[u], f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = activate<decltype(act)::value>(fmaf(f[i] - mean[i], mul[i], add[i]));
+            for (int i = 0; i < V; ++i) f[i] = activate<T, decltype(act)::value>(fmaf(f[i] - mean[i], mul[i], add[i]));
             Vec<T, V>::store(y + (size_t)row * a.c, f);
         }
     };
@@ -739,62 +752,191 @@ template <typename T, int V, bool WHOLE> tvg_status launch_once(const NormArgs &
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
+// The same for the backward pass: x and dy in registers.  The sums of a sample's channels go to the workspace ([n][c][2]), or,
+// of the only sample, to dgamma and dbeta.
+constexpr int kSumParts = 16;
+template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launch_bounds__(THREADS) void group_norm_grad_once_kernel(NormArgs a)
+{
+    extern __shared__ float lds[];
+    const int b = xcd_remap(blockIdx.x, a.tiles);
+    Tile t;
+    t.sample = b / a.blocks;
+    t.c0 = (b - t.sample * a.blocks) * a.block;
+    const int width = min(a.block, a.c - t.c0), cols = width / V, ng = width / a.cpg, g0 = t.c0 / a.cpg;
+    int col;
+    const int rp = THREADS / cols, lane_row = fast_div(threadIdx.x, cols, 1.0f / (float)cols, &col);
+    const bool active = lane_row < rp;
+    const int cc = col * V;
+    float *values = lds, *parts = lds + THREADS * V, *sums = parts + kSumParts * width, *group = sums + 2 * width;
+    const size_t at0 = ((size_t)t.sample * a.p) * a.c + t.c0 + cc;
+    const T *x = static_cast<const T *>(a.x) + at0, *dy = static_cast<const T *>(a.dy) + at0;
+    T *dx = static_cast<T *>(a.y) + at0;
+    typename Vec<T, V>::type rx[NV], rd[NV];
+    Channels<V, WHOLE> k;
+    if (active) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+            if (lane_row + u * rp < a.p) {
+                rx[u] = Vec<T, V>::load(x + (size_t)(lane_row + u * rp) * a.c);
+                rd[u] = Vec<T, V>::load(dy + (size_t)(lane_row + u * rp) * a.c);
+            }
+        k.load(a, t, g0, cc);
+    }
+    const auto rows = [&](auto act, auto &&f) {            // f(u, x, dz of i, which also gives d) of the lane's rows
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (lane_row + u * rp >= a.p) break;
+            float fx[V], fd[V];
+            Vec<T, V>::get(rx[u], fx);
+            Vec<T, V>::get(rd[u], fd);
+            f(u, fx, [&](int i, float &d) {
+                d = fx[i] - k.mean[i];
+                return activate_grad<T, decltype(act)::value>(fd[i], fmaf(d, k.mul[i], k.add[i]));
+            });
+        }
+    };
+    const auto with_act = [&](auto &&f) {
+        if (a.act == TVG_ACT_SILU) f(std::integral_constant<int, TVG_ACT_SILU>());
+        else if (a.act == TVG_ACT_RELU) f(std::integral_constant<int, TVG_ACT_RELU>());
+        else f(std::integral_constant<int, TVG_ACT_NONE>());
+    };
+    float s[2][V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[0][i] = s[1][i] = 0.0f;
+    if (active)
+        with_act([&](auto act) {
+            rows(act, [&](int, float (&)[V], auto &&dz_of) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float d;
+                    const float dz = dz_of(i, d);
+                    s[0][i] += dz;
+                    s[1][i] = fmaf(dz, d, s[1][i]);
+                }
+            });
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[1][i] *= k.rstd[i];
+        });
+    const int lanes = min(kSumParts, rp);
+    int c;
+    const int part = fast_div(threadIdx.x, width, 1.0f / (float)width, &c);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) values[lane_row * width + cc + i] = s[q][i];
+        }
+        __syncthreads();
+        // a channel's lanes by `lanes` threads, then those
+        const int stride = max(1, min(lanes, THREADS / width));
+        for (int c1 = c, p1 = part; c1 < width && p1 < stride; c1 += width <= THREADS ? width : THREADS) {
+            float v = 0.0f;
+#pragma unroll 4
+            for (int r = p1; r < rp; r += stride) v += values[r * width + c1];
+            parts[p1 * width + c1] = v;
+        }
+        __syncthreads();
+        for (int c1 = threadIdx.x; c1 < width; c1 += THREADS) {
+            float v = 0.0f;
+            for (int r = 0; r < stride; ++r) v += parts[r * width + c1];
+            sums[q * width + c1] = v;
+        }
+        __syncthreads();
+    }
+    for (int c1 = threadIdx.x; c1 < width; c1 += THREADS) {
+        const float v1 = sums[c1], v2 = sums[width + c1];
+        if (a.n > 1) {
+            reinterpret_cast<float2 *>(a.chan)[(size_t)t.sample * a.c + t.c0 + c1] = float2{v1, v2};
+        } else {
+            if (a.dbeta) a.dbeta[t.c0 + c1] = v1;
+            if (a.dgamma) a.dgamma[t.c0 + c1] = v2;
+        }
+    }
+    {
+        const int team = threadIdx.x / kPairTeam, tl = threadIdx.x % kPairTeam;
+        const float inv = 1.0f / ((float)a.p * (float)a.cpg);
+        for (int g = team; g < ng; g += THREADS / kPairTeam) {
+            float v1 = 0.0f, v2 = 0.0f;
+            for (int i = tl; i < a.cpg; i += kPairTeam) {
+                const int c1 = g * a.cpg + i;
+                const float gm = a.gamma ? a.gamma[t.c0 + c1] : 1.0f;
+                v1 = fmaf(gm, sums[c1], v1);
+                v2 = fmaf(gm, sums[width + c1], v2);
+            }
+            v1 = team_sum<kPairTeam>(v1);
+            v2 = team_sum<kPairTeam>(v2);
+            if (tl == 0) {
+                group[2 * g] = v1 * inv;
+                group[2 * g + 1] = v2 * inv;
+            }
+        }
+    }
+    __syncthreads();
+    if (!active) return;
+    float sa[V], sb[V];
+    for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
+        sa[i] = group[2 * g] * k.rstd[i];
+        sb[i] = group[2 * g + 1] * (k.rstd[i] * k.rstd[i]);
+    });
+    with_act([&](auto act) {
+        rows(act, [&](int u, float (&fx)[V], auto &&dz_of) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float d;
+                const float dz = dz_of(i, d);
+                fx[i] = fmaf(dz, k.mul[i], -fmaf(d, sb[i], sa[i]));
+            }
+            Vec<T, V>::store(dx + (size_t)(lane_row + u * rp) * a.c, fx);
+        });
+    });
+}
+
+__global__ __launch_bounds__(kThreads) void group_norm_reduce_kernel(NormArgs a, int rows)
+{
+    __shared__ float lds[2 * kThreads];
+    reduce_channels(a, rows, blockIdx.x * kReduceChannels, lds);
+}
+
+template <typename T, int V, bool WHOLE> tvg_status launch_grad_once(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    const size_t lds = ((size_t)plan.threads * V + (kSumParts + 2) * a.block + 2 * (a.block / a.cpg)) * sizeof(float);
+    if (plan.threads == 256) hipLaunchKernelGGL((group_norm_grad_once_kernel<T, V, 2, 256, WHOLE>), dim3(a.tiles), dim3(256), lds, stream, a);
+    else if (plan.threads == 512) hipLaunchKernelGGL((group_norm_grad_once_kernel<T, V, 4, 512, WHOLE>), dim3(a.tiles), dim3(512), lds, stream, a);
+    else hipLaunchKernelGGL((group_norm_grad_once_kernel<T, V, 8, 1024, WHOLE>), dim3(a.tiles), dim3(1024), lds, stream, a);
+    if (a.n > 1 && (a.dgamma || a.dbeta))
+        hipLaunchKernelGGL(group_norm_reduce_kernel, dim3((a.c + kReduceChannels - 1) / kReduceChannels), dim3(kThreads), 0, stream, a, a.n);
+    return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
+}
+
 // Whether a lane's channels are always of one group.
 template <int V> bool whole_vectors(const NormArgs &a) { return a.cpg % V == 0; }
 
-// The arguments of samples n0 to n0 + n.
-NormArgs samples(const NormArgs &a, int n0, int n, size_t elem)
+template <typename T, int V, bool WHOLE> tvg_status launch_forward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
 {
-    NormArgs b = a;
-    const size_t at = (size_t)n0 * a.p * a.c * elem;
-    b.x = static_cast<const char *>(a.x) + at;
-    b.y = static_cast<char *>(a.y) + at;
-    if (a.dy) b.dy = static_cast<const char *>(a.dy) + at;
-    if (a.mean) b.mean += (size_t)n0 * a.groups;
-    if (a.rstd) b.rstd += (size_t)n0 * a.groups;
-    b.part += (size_t)n0 * a.groups * a.chunks * 2;
-    if (a.chan) b.chan += (size_t)n0 * a.chunks * a.c * 2;
-    b.n = n;
-    b.tiles = n * a.blocks * a.chunks;
-    return b;
-}
-
-template <typename T, int V, bool WHOLE> tvg_status launch_forward(const NormArgs &all, const NormPlan &plan, hipStream_t stream)
-{
-    if (plan.once) return launch_once<T, V, WHOLE>(all, plan, stream);
-    for (int n0 = 0; n0 < all.n; n0 += plan.batch) {
-        const NormArgs a = samples(all, n0, std::min(plan.batch, all.n - n0), sizeof(T));
-        const dim3 grid(a.tiles), threads(kThreads);
-        hipLaunchKernelGGL((group_norm_stats_kernel<T, V, WHOLE>), grid, threads, plan.lds_stats, stream, a);
-        if (a.act == TVG_ACT_SILU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_SILU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
-        else if (a.act == TVG_ACT_RELU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_RELU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
-        else hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_NONE, WHOLE>), grid, threads, plan.lds_apply, stream, a);
-        if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
-    }
-    return TVG_OK;
+    if (plan.once) return launch_once<T, V, WHOLE>(a, plan, stream);
+    const dim3 grid(a.tiles), threads(kThreads);
+    hipLaunchKernelGGL((group_norm_stats_kernel<T, V, WHOLE>), grid, threads, plan.lds_stats, stream, a);
+    if (a.act == TVG_ACT_SILU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_SILU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+    else if (a.act == TVG_ACT_RELU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_RELU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+    else hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_NONE, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+    return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 template <typename T, int V> tvg_status launch_forward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
 {
     return whole_vectors<V>(a) ? launch_forward<T, V, true>(a, plan, stream) : launch_forward<T, V, false>(a, plan, stream);
 }
 
-template <typename T, int V, int ACT, bool WHOLE> tvg_status launch_grad(const NormArgs &all, const NormPlan &plan, hipStream_t stream)
+template <typename T, int V, int ACT, bool WHOLE> tvg_status launch_grad(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
 {
-    for (int n0 = 0; n0 < all.n; n0 += plan.batch) {
-        const NormArgs a = samples(all, n0, std::min(plan.batch, all.n - n0), sizeof(T));
-        // (the last launch has the sums of all samples)
-        const bool last = n0 + plan.batch >= all.n;
-        const int reducers = last && (a.dgamma || a.dbeta) ? (a.c + kReduceChannels - 1) / kReduceChannels : 0;
-        hipLaunchKernelGGL((group_norm_grad_sums_kernel<T, V, ACT, WHOLE>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
-        hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a,
-                           reducers, all.chan, all.n * all.chunks);
-        if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
-    }
-    return TVG_OK;
+    const int reducers = a.dgamma || a.dbeta ? (a.c + kReduceChannels - 1) / kReduceChannels : 0;
+    hipLaunchKernelGGL((group_norm_grad_sums_kernel<T, V, ACT, WHOLE>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
+    hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a, reducers);
+    return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
 template <typename T, int V, bool WHOLE> tvg_status launch_backward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
 {
+    if (plan.once) return launch_grad_once<T, V, WHOLE>(a, plan, stream);
     if (a.act == TVG_ACT_SILU) return launch_grad<T, V, TVG_ACT_SILU, WHOLE>(a, plan, stream);
     if (a.act == TVG_ACT_RELU) return launch_grad<T, V, TVG_ACT_RELU, WHOLE>(a, plan, stream);
     return launch_grad<T, V, TVG_ACT_NONE, WHOLE>(a, plan, stream);
@@ -840,22 +982,24 @@ NormArgs make_args(const NormProblem &p, const NormPlan &plan)
 
 // The plan of one launch, if a block of channels fits a workgroup's registers: blocks for a workgroup a CU, 64 bytes of a row
 // at least where that fits, 32 at least.
-static bool plan_once(const NormProblem &p, int vector, NormPlan *plan)
+static bool plan_once(const NormProblem &p, int vector, bool backward, NormPlan *plan)
 {
     const int cpg = p.c / p.groups, size = p.dtype == TVG_BF16 ? 2 : 4;
     const int unit = cpg / gcd(cpg, vector) * vector;                  // divides c: so do both
-    static const int kLanes[3] = {256, 512, 1024}, kVectors[3] = {4, 8, 16};
+    static const int kLanes[3] = {256, 512, 1024}, kVectors[2][3] = {{4, 8, 16}, {2, 4, 8}};
     const auto fits = [&](int width, int k) {
         const int cols = width / vector;
-        return cols <= kLanes[k] && width / cpg <= 2048 && ((int64_t)p.p + kLanes[k] / cols - 1) / (kLanes[k] / cols) <= kVectors[k];
+        // (LDS: 32 KB of sums, and of the backward pass 20 floats a channel)
+        return cols <= kLanes[k] && width / cpg <= 2048 && (!backward || width <= 384) &&
+               ((int64_t)p.p + kLanes[k] / cols - 1) / (kLanes[k] / cols) <= kVectors[backward][k];
     };
     int64_t units = std::max<int64_t>((int64_t)p.n * p.c / kComputeUnits / unit, (64 / size + unit - 1) / unit);
     units = std::min<int64_t>(units, p.c / unit);
     while (units > 1 && !fits((int)units * unit, 2)) --units;
     const int width = (int)units * unit;
     // (few workgroups with much each: the two launches spread it)
-    if ((int64_t)p.n * ((p.c + width - 1) / width) < kComputeUnits / 2 && (int64_t)p.p * width * size > 32 * 1024) return false;
-    if (!fits(width, 2) || (width * size < 32 && width < p.c)) return false;
+    if ((int64_t)p.n * ((p.c + width - 1) / width) < kComputeUnits / 2 && (int64_t)p.p * width * size > (backward ? 16 : 32) * 1024) return false;
+    if (!fits(width, 2) || (width * size < (backward ? 64 : 32) && width < p.c)) return false;
     int k = 0;
     while (!fits(width, k)) ++k;
     plan->once = true;
@@ -864,34 +1008,35 @@ static bool plan_once(const NormProblem &p, int vector, NormPlan *plan)
     plan->blocks = (p.c + width - 1) / width;
     plan->rows = p.p;
     plan->chunks = 1;
-    plan->part_floats = plan->chan_floats = 0;
+    plan->part_floats = 0;
+    plan->chan_floats = backward && p.n > 1 ? (size_t)p.n * p.c * 2 : 0;
     return true;
 }
 
-constexpr int64_t kBatchBytes = (int64_t)100 << 40;
 
-// Row chunks: as many workgroups as keep every CU busy, with eight vectors a lane at least and 64 chunks of a sample at
-// most, whose statistics every workgroup of the second launch joins.
+// Row chunks: two workgroups a CU with four vectors a lane at least, or one with two.  Every workgroup of the second launch joins
+// the statistics of its sample's chunks, 64 of them in one round of loads: more only where a chunk would have more than 48 KB
+// (one map 300x300x64: 64 chunks 32 us, 240 23 us; one map 56x56x256: 64 chunks 13.4 us, 196 15.1 us).  8 maps 64x64x320: two
+// workgroups a CU 24.3 us, four 31.5, eight 44.
 static void plan_group_norm(const NormProblem &p, int vector, bool backward, NormPlan *plan)
 {
     const int cpg = p.c / p.groups;
     plan->once = false;
     plan->vector = vector;
-    if (!backward && plan_once(p, vector, plan)) return;
+    if (plan_once(p, vector, backward, plan)) return;
     // a block of whole groups and whole vectors, as wide as one pass of the workgroup
     const int64_t unit = (int64_t)cpg * vector / gcd(cpg, vector);
-    const int64_t most = (int64_t)kThreads * vector;
+    const int64_t widest = (int64_t)kThreads * vector;
     plan->vector = vector;
-    plan->block = unit >= p.c ? p.c : p.c <= most ? p.c : (int)(unit * std::max<int64_t>(1, most / unit));
+    plan->block = unit >= p.c ? p.c : p.c <= widest ? p.c : (int)(unit * std::max<int64_t>(1, widest / unit));
     plan->blocks = (p.c + plan->block - 1) / plan->block;
     const int cols = std::min(plan->block / vector, kThreads), rp = kThreads / cols;
-    // Samples at a time: what the first launch reads is in the memory-side cache (256 MB) when the second reads it again.
-    const int64_t sample = (int64_t)p.p * p.c * (p.dtype == TVG_BF16 ? 2 : 4) * (backward ? 2 : 1);
-    const int most_at_once = (int)std::min<int64_t>(p.n, std::max<int64_t>(1, kBatchBytes / sample));
-    const int batches = (p.n + most_at_once - 1) / most_at_once;
-    plan->batch = (p.n + batches - 1) / batches;
-    const int64_t want = std::max<int64_t>(1, 8 * kComputeUnits / ((int64_t)plan->batch * plan->blocks));
-    int64_t chunks = std::min<int64_t>(std::min<int64_t>(want, 64), std::max<int64_t>(1, p.p / (8 * rp)));
+    const int64_t others = (int64_t)p.n * plan->blocks, sample = (int64_t)p.p * p.c * (p.dtype == TVG_BF16 ? 2 : 4) * (backward ? 2 : 1);
+    const int64_t most = std::min<int64_t>(256, std::max<int64_t>(kPairChunks, sample / (48 * 1024)));
+    const auto chunks_of = [&](int per_cu, int rows) {
+        return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(per_cu * kComputeUnits / others, most), p.p / (rows * rp)));
+    };
+    const int64_t chunks = std::max(chunks_of(2, 4), chunks_of(1, 2));
     plan->rows = (int)((p.p + chunks - 1) / chunks);
     plan->chunks = (p.p + plan->rows - 1) / plan->rows;
     const int groups = plan->block / cpg;

@@ -460,10 +460,10 @@ __device__ __forceinline__ void multiply_adapter(M &&has_it, const uint4v (&bv)[
     }
 }
 
-__device__ __forceinline__ float lora_act(float t, int act)
+template <typename T> __device__ __forceinline__ float lora_act(float t, int act)
 {
     if (act == TVG_ACT_RELU) return t < 0.0f ? 0.0f : t;               // (a NaN stays one)
-    if (act == TVG_ACT_SILU) return t * sigmoid(t);
+    if (act == TVG_ACT_SILU) return t * sigmoid<sizeof(T) == 4>(t);
     return t;
 }
 
@@ -521,7 +521,7 @@ __device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, cons
                 }
                 if (a.act != TVG_ACT_NONE) {
 #pragma unroll
-                    for (int v = 0; v < E; ++v) f[v] = lora_act(f[v], a.act);
+                    for (int v = 0; v < E; ++v) f[v] = lora_act<T>(f[v], a.act);
                 }
                 uint4v out;
 #pragma unroll
@@ -539,7 +539,7 @@ __device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, cons
                 const size_t at = (size_t)row * a.k + c1;
                 float f = stage[t * kRow + lane % kLanes1] + bias[0];
                 if (res) f += Elem<T>::load(res + at, 0);
-                Elem<T>::store(y + at, 0, lora_act(f, a.act));
+                Elem<T>::store(y + at, 0, lora_act<T>(f, a.act));
             }
         }
     }
@@ -604,7 +604,7 @@ template <typename T> __device__ __forceinline__ void store4(const LoraArgs &a, 
         float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (res) Group4<T>::unpack(*reinterpret_cast<const gvec *>(res + at), r);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) f[v] = lora_act(t[v] + (a.bias ? a.bias[ch + v] : 0.0f) + r[v], a.act);
+        for (int v = 0; v < 4; ++v) f[v] = lora_act<T>(t[v] + (a.bias ? a.bias[ch + v] : 0.0f) + r[v], a.act);
         *reinterpret_cast<gvec *>(y + at) = Group4<T>::pack(f);
         return;
     }
@@ -612,7 +612,7 @@ template <typename T> __device__ __forceinline__ void store4(const LoraArgs &a, 
     for (int v = 0; v < 4; ++v)
         if (ch + v < a.k) {
             f[v] = t[v] + (a.bias ? a.bias[ch + v] : 0.0f) + (res ? Elem<T>::load(res + at, v) : 0.0f);
-            Elem<T>::store(y + at, v, lora_act(f[v], a.act));
+            Elem<T>::store(y + at, v, lora_act<T>(f[v], a.act));
         }
 }
 

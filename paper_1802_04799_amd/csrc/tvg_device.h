@@ -117,9 +117,11 @@ __device__ __forceinline__ float relu_floor(bool relu)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(relu ? 0u : 0x7FC00000u));
 }
 
-// 1 / (1 + exp(-z)).  exp2 of z log2(e) in two parts: the product's rounding alone would cost |z| half steps.
-__device__ __forceinline__ float sigmoid(float z)
+// 1 / (1 + exp(-z)).  PRECISE: exp2 of z log2(e) in two parts, since the product's rounding alone costs |z| half steps of fp32;
+// values that are rounded to bf16 do without.
+template <bool PRECISE> __device__ __forceinline__ float sigmoid(float z)
 {
+    if constexpr (!PRECISE) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269502f * z));
     const float c = fmaxf(z, -87.0f);                      // (exp stays finite; sigmoid is below 2^-125 there)
     const float t = -1.44269502f * c;
     const float lo = fmaf(-1.44269502f, c, -t) - 1.92596299e-8f * c;

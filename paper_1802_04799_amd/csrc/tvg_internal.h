@@ -274,7 +274,6 @@ struct NormPlan {
     int vector;                       // channels per lane
     bool once;                        // one launch, of `threads` lanes a workgroup
     int threads;
-    int batch;                        // samples per pair of launches
     int block, blocks;                // channels per workgroup, workgroups across the channels
     int rows, chunks;                 // rows per workgroup, workgroups across the rows
     size_t lds_stats, lds_apply;

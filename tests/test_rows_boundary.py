@@ -87,7 +87,7 @@ def test_pointers_workspaces_and_alignment():
         assert tvg.tvg_linear_lora_fused(d, *[p] * 9, ws, size, 0) == 4
     assert tvg.tvg_linear_lora_fused(lora(rows=0), *[0] * 9, 0, 0, 0) == 0          # nothing to do
     assert tvg.tvg_linear_lora_workspace_size(lora(rows=0)) == 0
-    assert tvg.tvg_linear_lora_workspace_size(lora(adapters=0)) == 0
+    assert tvg.tvg_linear_lora_workspace_size(lora(adapters=0)) < need
     lib = tvg.load()
     assert lib.tvg_group_norm_workspace_size(None, ctypes.byref(ctypes.c_size_t())) == 1
     assert lib.tvg_linear_lora_workspace_size(ctypes.byref(d), None) == 1
