@@ -752,7 +752,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rsel = lane & 15, quad = lane >> 4;
-    const int row0 = tm * TM, ch0 = tn * TN, wr = wave % WR * (TM / WR), wc = wave / WR * (TN / WC);
+    const int row0 = tm * TM, ch0 = tn * TN, wr = wave / WC * (TM / WR), wc = wave % WC * (TN / WC);
     const uint32_t row_bytes = (uint32_t)a.c * sizeof(T);
     // (rows in order of their adapters: anywhere in x, whose bytes 32 bits count then)
     const int base = a.order ? 0 : row0, reach = a.order ? a.rows : min(TM, a.rows - row0);
@@ -785,6 +785,34 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         for (int e = 0; e < kPer16<T>; ++e) to_b[e] = ch0 + row < a.k && r0 + e < a.rank ? from_b[e] : (T)0;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
+    // Tiles of several adapters: a step of the ring is a block of 16 ranks of h and of B of the next kBGroup adapters.
+    constexpr int kBRow = sizeof(T) == 2 && TN > 64 ? 32 : 64;         // bytes of a row of B (bf16, 64: its 16 ranks twice)
+    constexpr int kBLoads = TN * kBRow / 1024 / W, kBStage = TN * kBRow, kBGroup = (kLoads - kLoadsX) / kBLoads;
+    static_assert(kBLoads * W * 1024 == kBStage && kBGroup * kBLoads == kLoads - kLoadsX, "as many loads a step as the product has");
+    int next_at = 0, next_block = 0;
+    const auto fetch_h = [&](uint32_t to, int j, bool any) {
+        const uint4v hbuf = raw_buffer(a.h + (size_t)base * a.rblocks * 64, (uint32_t)reach * a.rblocks * 64);
+#pragma unroll
+        for (int n = 0; n < kLoadsX; ++n) {
+            const int row = (n * W + wave) * 16 + lrow;
+            const uint32_t at = ((row_of[row] - base) * a.rblocks + j) * 64 + piece * 16;
+            load_to_lds(to + n * W * 1024, any && row0 + row < a.rows ? at : kBeyond, hbuf, 0);
+        }
+    };
+    const auto fetch_b = [&](int to, int at) {
+        const bool any = next_block < a.rblocks && at < adapters;
+        const int i = any ? __builtin_amdgcn_readfirstlane(list[at]) : 0;
+        const uint4v bbuf = raw_buffer(static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0) * a.rank,
+                                       (uint32_t)min(TN, a.k - ch0) * a.rank * (uint32_t)sizeof(T));
+#pragma unroll
+        for (int l = 0; l < kBLoads; ++l) {
+            const int row = ((l * W + wave) * 1024 + lane * 16) / kBRow;
+            const uint32_t r = sizeof(T) == 2 ? next_block * 32 + (lane & 1) * 16 : next_block * 64 + (lane & 3) * 16;
+            const bool ok = any && ch0 + row < a.k && r < a.rank * sizeof(T);
+            if (a.wide_rank || !any) load_to_lds(lds0 + to + l * W * 1024, ok ? row * a.rank * (uint32_t)sizeof(T) + r : kBeyond, bbuf, 0);
+            else copy_b(i, row, (int)(r / sizeof(T)), to + l * W * 1024);
+        }
+    };
     const auto fetch_any = [&](int s) {
         const uint32_t to = lds0 + (s & (RING - 1)) * kStage + wave * 1024;
         if (s < turns) {
@@ -795,21 +823,29 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
             }
             return;
         }
+        if (adapters > 0 && blocks == 0) {
+            fetch_h(to, next_block, next_block < a.rblocks);
+#pragma unroll
+            for (int q = 0; q < kBGroup; ++q) fetch_b((s & (RING - 1)) * kStage + TM * kSlice + q * kBStage + wave * 1024, next_at + q);
+            next_at += kBGroup;
+            if (next_at >= adapters) {
+                next_at = 0;
+                ++next_block;
+            }
+            return;
+        }
         // a block of 16 ranks of the only adapter: h of the tokens, and B, whose 16 ranks bf16 takes twice
         const bool any = fetched < blocks;
         const int i = any ? __builtin_amdgcn_readfirstlane(list[0]) : 0;
-        const uint4v hbuf = raw_buffer(a.h + (size_t)base * a.rblocks * 64, (uint32_t)reach * a.rblocks * 64);
+        fetch_h(to, fetched, any);
         const uint4v bbuf = raw_buffer(static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0) * a.rank,
                                        (uint32_t)min(TN, a.k - ch0) * a.rank * (uint32_t)sizeof(T));
         const uint32_t bpiece = sizeof(T) == 2 ? fetched * 32 + (piece & 1) * 16 : fetched * 64 + piece * 16;
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const int row = (n < kLoadsX ? n * W + wave : (n - kLoadsX) * W + wave) * 16 + lrow;
-            const int end = n < kLoadsX ? min(TM, a.rows - row0) : min(TN, a.k - ch0);
-            uint32_t at = n < kLoadsX ? ((row_of[row & (TM - 1)] - base) * a.rblocks + fetched) * 64 + piece * 16
-                                      : row * a.rank * (uint32_t)sizeof(T) + bpiece;
-            if (!any || row >= end || (n >= kLoadsX && bpiece >= a.rank * sizeof(T))) at = kBeyond;
-            if (n < kLoadsX || a.wide_rank || !any) load_to_lds(to + n * W * 1024, at, n < kLoadsX ? hbuf : bbuf, 0);
+        for (int n = kLoadsX; n < kLoads; ++n) {
+            const int row = ((n - kLoadsX) * W + wave) * 16 + lrow;
+            const bool ok = any && ch0 + row < a.k && bpiece < a.rank * sizeof(T);
+            if (a.wide_rank || !any) load_to_lds(to + n * W * 1024, ok ? row * a.rank * (uint32_t)sizeof(T) + bpiece : kBeyond, bbuf, 0);
             else copy_b(i, row, (int)(bpiece / sizeof(T)), (int)(to - lds0) + n * W * 1024);
         }
         ++fetched;
@@ -890,6 +926,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         step(s, xv[0], wv[0], xv[1], wv[1]);
         step(s + 1, xv[1], wv[1], xv[0], wv[0]);
     }
+    const bool mixed = adapters > 0 && blocks == 0;
     // the last slices, then, where all tokens have the same adapter, its blocks of ranks
 #pragma unroll 1
     for (const int end = turns + blocks; s < end; ++s) {
@@ -898,61 +935,29 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         read(s, xv[0], wv[0]);
         multiply(xv[0], wv[0]);
     }
-    if (adapters > 0 && blocks == 0) {
-        // Several adapters: a block of ranks of h stays in registers while B of every adapter comes through the ring, deeper
-        // than before since it is B alone.
-        constexpr int kRow = sizeof(T) == 2 && TN > 64 ? 32 : 64;      // bytes of a row of B (bf16, 64: its 16 ranks twice)
-        constexpr int kBLoads = TN * kRow / 1024 / W, kBStage = TN * kRow, kBRing = 8;
-        static_assert(kBLoads * W * 1024 == TN * kRow && kBRing * kBStage <= RING * kStage, "whole loads of every wave, in the ring's place");
-        const int total = adapters * a.rblocks;
-        int next = 0, next_at = 0, next_block = 0;
-        const auto fetch_b = [&] {
-            const bool any = next < total;
-            const int i = any ? __builtin_amdgcn_readfirstlane(list[next_at]) : 0;
-            const uint4v bbuf = raw_buffer(static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0) * a.rank,
-                                           (uint32_t)min(TN, a.k - ch0) * a.rank * (uint32_t)sizeof(T));
-            const uint32_t to = (next & (kBRing - 1)) * kBStage + wave * 1024;
-#pragma unroll
-            for (int l = 0; l < kBLoads; ++l) {
-                const int byte = (l * W + wave) * 1024 + lane * 16, row = byte / kRow;
-                const uint32_t r = sizeof(T) == 2 ? next_block * 32 + (lane & 1) * 16 : next_block * 64 + (lane & 3) * 16;
-                const bool ok = any && ch0 + row < a.k && r < a.rank * sizeof(T);
-                if (a.wide_rank || !any) load_to_lds(lds0 + to + l * W * 1024, ok ? row * a.rank * (uint32_t)sizeof(T) + r : kBeyond, bbuf, 0);
-                else copy_b(i, row, (int)(r / sizeof(T)), (int)to + l * W * 1024);
-            }
-            ++next;
-            if (++next_at == adapters) {
-                next_at = 0;
-                ++next_block;
-            }
-        };
-        wait_loads<0>();
-        __builtin_amdgcn_s_barrier();                      // (all waves have read the ring)
-        asm volatile("" ::: "memory");
-#pragma unroll 1
-        for (int d = 0; d < kBRing - 1; ++d) fetch_b();
-        int mine[NB];
+    if (mixed) {
+        int mine[NB], at = 0, j = 0;
 #pragma unroll
         for (int n = 0; n < NB; ++n) mine[n] = ids[wr + n * 16 + rsel];
-        const int bat = (wc + rsel) * kRow + (sizeof(T) == 2 ? quad & 1 : quad) * 16;
-        int e = 0;
+        const int bat = (wc + rsel) * kBRow + (sizeof(T) == 2 && kBRow == 32 ? quad & 1 : quad) * 16;
 #pragma unroll 1
-        for (int j = 0; j < a.rblocks; ++j) {
-            uint4v hv[NB];
+        for (; j < a.rblocks; ++s) {
+            behind();
+            fetch_any(s + RING - 1);
+            const unsigned char *p = lds + (s & (RING - 1)) * kStage;
 #pragma unroll
-            for (int n = 0; n < NB; ++n) hv[n] = load_h(a, min(row_of[wr + n * 16 + rsel], a.rows - 1), j, quad);
+            for (int n = 0; n < NB; ++n) xv[0][n] = *reinterpret_cast<const uint4v *>(p + xat + n * 16 * kSlice);
 #pragma unroll 1
-            for (int at = 0; at < adapters; ++at, ++e) {
-                wait_loads<(kBRing - 2) * kBLoads>();
-                __builtin_amdgcn_s_barrier();
-                __builtin_amdgcn_sched_barrier(0);
-                fetch_b();
+            for (int q = 0; q < kBGroup && at < adapters; ++q, ++at) {
                 const int i = __builtin_amdgcn_readfirstlane(list[at]);
-                const unsigned char *p = lds + (e & (kBRing - 1)) * kBStage + bat;
-                uint4v bv[MB];
 #pragma unroll
-                for (int m = 0; m < MB; ++m) bv[m] = *reinterpret_cast<const uint4v *>(p + m * 16 * kRow);
-                multiply_adapter<T>([&](int n) { return mine[n] == i; }, bv, [&](int n) { return hv[n]; }, acc);
+                for (int m = 0; m < MB; ++m) wv[0][m] = *reinterpret_cast<const uint4v *>(p + TM * kSlice + q * kBStage + bat + m * 16 * kBRow);
+                multiply_adapter<T>([&](int n) { return mine[n] == i; }, wv[0],
+                                    [&](int n) { return xv[0][n]; }, acc);
+            }
+            if (at == adapters) {
+                at = 0;
+                ++j;
             }
         }
     }
