@@ -105,6 +105,9 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const
 // until at most N younger memory operations are in flight
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
+// until no LDS operation is in flight
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 constexpr uint32_t kBeyond = 0x80000000u;  // an offset outside of every buffer: a load returns zeros
 
 // The product of 16 MB rows of w and 16 NB rows of x over a part of the reduction, by one wave: 128 bytes of every row at a
@@ -162,7 +165,7 @@ template <typename T, int MB, int NB, int DEPTH> struct WaveProduct {
 #pragma unroll
                 for (int m = 0; m < MB; ++m) w[s][m] = *reinterpret_cast<const uint4v *>(p + (NB + m) * 2048 + o);
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_reads();
             fetch(c + DEPTH * step, slot);
 #pragma unroll
             for (int s = 0; s < 2; ++s) mma_all(w[s], x[s], acc, T());
@@ -777,13 +780,15 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load_to_lds(to + i * W * 1024, from[i], i < kLoadsX ? xbuf : wbuf, s * kSlice);
     };
-    // 16 bytes a lane of a row of B at any element: through registers (whose loads are younger than the step's own, and waited for)
+    // 16 bytes a lane of a row of B at any element: through registers.  (It waits for all loads: such a step has fewer than
+    // kLoads in flight, or none of B where all channels of the wave lie beyond the last.)
     const auto copy_b = [&](int i, int row, int r0, int to) {
         const T *from_b = static_cast<const T *>(a.b) + ((size_t)i * a.k + ch0 + row) * a.rank + r0;
         T *to_b = reinterpret_cast<T *>(lds + to + lane * 16);
 #pragma unroll 1
         for (int e = 0; e < kPer16<T>; ++e) to_b[e] = ch0 + row < a.k && r0 + e < a.rank ? from_b[e] : (T)0;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_loads<0>();
+        wait_reads();
     };
     // Tiles of several adapters: a step of the ring is a block of 16 ranks of h and of B of the next kBGroup adapters.
     constexpr int kBRow = sizeof(T) == 2 && TN > 64 ? 32 : 64;         // bytes of a row of B (bf16, 64: its 16 ranks twice)
@@ -887,7 +892,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
 #pragma unroll 1
     for (int i = 0; i < RING - 1; ++i) {
         if (i == 2 && a.adapters > 0) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_reads();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (wave == 0) {
@@ -909,7 +914,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
                     list[TM + 1] = same;
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_reads();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             adapters = __builtin_amdgcn_readfirstlane(list[TM]);
@@ -933,6 +938,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         behind();
         fetch_any(s + RING - 1);
         read(s, xv[0], wv[0]);
+        wait_reads();                      // (the next step's barrier lets other waves write there)
         multiply(xv[0], wv[0]);
     }
     if (mixed) {
@@ -955,6 +961,7 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
                 multiply_adapter<T>([&](int n) { return mine[n] == i; }, wv[0],
                                     [&](int n) { return xv[0][n]; }, acc);
             }
+            wait_reads();
             if (at == adapters) {
                 at = 0;
                 ++j;

@@ -83,6 +83,20 @@ def test_projection(tvg, rows, c, k, rank, adapters, dtype):
     check(tvg, make(rows, c, k, rank, adapters, dtype, seed, residual=True, bias=True, scale=False), ("relu", "silu")[seed % 2], dtype)
 
 
+# ... of many tiles: 64, 128 and 256 rows and channels a tile (bf16; fp32 up to 128), ragged at both ends, reductions shorter
+# than a step, ranks that are not whole 16-byte pieces, rows at any element
+LARGE = [(1100, 72, 1100, 16, 5), (1100, 1000, 1100, 12, 9), (300, 64, 6000, 256, 2), (2100, 72, 2060, 40, 7), (2048, 8, 2048, 8, 3),
+         (2048, 200, 2049, 5, 11), (4100, 136, 2600, 16, 30), (4100, 520, 2600, 72, 30), (4097, 40, 2570, 4, 3), (1100, 37, 1100, 7, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,k,rank,adapters", LARGE)
+def test_large_projection(tvg, rows, c, k, rank, adapters, dtype):
+    seed = rows + c + k + rank
+    check(tvg, make(rows, c, k, rank, adapters, dtype, seed), None, dtype)
+    check(tvg, make(rows, c, k, rank, adapters, dtype, seed, residual=True, bias=True, scale=False), ("relu", "silu")[seed % 2], dtype)
+
+
 def assignments(rows, adapters):
     """Rows of requests of many kinds: one adapter, none, long runs, single rows, unsorted, indices out of range."""
     import torch
@@ -96,7 +110,8 @@ def assignments(rows, adapters):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,c,k,rank,adapters", [(40, 512, 192, 16, 40), (300, 256, 320, 8, 6), (1100, 128, 520, 32, 9), (7, 1024, 64, 20, 3)])
+@pytest.mark.parametrize("rows,c,k,rank,adapters", [(40, 512, 192, 16, 40), (300, 256, 320, 8, 6), (1100, 128, 520, 32, 9), (7, 1024, 64, 20, 3),
+                                                      (1100, 136, 1100, 16, 40), (2100, 72, 2060, 32, 5000), (4100, 72, 2600, 24, 60)])
 def test_assignments(tvg, rows, c, k, rank, adapters, dtype):
     p = make(rows, c, k, rank, adapters, dtype, rows)
     for name, index in assignments(rows, adapters).items():
@@ -105,11 +120,11 @@ def test_assignments(tvg, rows, c, k, rank, adapters, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [1, 6, 50, 300, 1100])
-def test_a_row_does_not_see_the_adapters_of_others(tvg, rows, dtype):
+@pytest.mark.parametrize("rows,k", [(1, 264), (6, 264), (50, 264), (300, 264), (1100, 264), (1100, 1100), (2100, 2060), (4100, 2600)])
+def test_a_row_does_not_see_the_adapters_of_others(tvg, rows, k, dtype):
     """Adapters full of infinities and NaN, and rows of x too: the other rows keep their bits."""
     import torch
-    p = make(rows, 256, 264, 16, 4, dtype, rows)
+    p = make(rows, 256, k, 16, 4, dtype, rows)
     call = lambda: tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"])
     clean = call()
     keep = p["adapter"] != 2
@@ -140,20 +155,20 @@ def test_infinite_middle_vectors_stay_infinite(tvg):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [3, 40, 300])
-def test_any_alignment_and_surroundings(tvg, rows, dtype):
+@pytest.mark.parametrize("rows,k", [(3, 136), (40, 136), (300, 136), (1100, 1096), (2100, 2056), (4100, 2600)])
+def test_any_alignment_and_surroundings(tvg, rows, k, dtype):
     """Operands that start at any element: the same result within the tolerance, and nothing beside y is written."""
     import torch
-    p = make(rows, 256, 136, 16, 3, dtype, 77, residual=True, bias=True)
+    p = make(rows, 256, k, 16, 3, dtype, 77, residual=True, bias=True)
     check(tvg, p, "silu", dtype)
     for name in ("x", "w", "a", "b", "residual"):
         t = p[name]
         room = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")
         p[name] = room[1:1 + t.numel()].view(t.shape).copy_(t)
-        room = torch.full((rows * 136 + 16,), 7.0, dtype=t.dtype, device="cuda")
-        out = room[3:3 + rows * 136].view(rows, 136)
+        room = torch.full((rows * k + 16,), 7.0, dtype=t.dtype, device="cuda")
+        out = room[3:3 + rows * k].view(rows, k)
         check(tvg, p, "silu", dtype, out=out)
-        assert bool((room[:3] == 7).all()) and bool((room[3 + rows * 136:] == 7).all())
+        assert bool((room[:3] == 7).all()) and bool((room[3 + rows * k:] == 7).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -171,12 +186,12 @@ def test_no_adapters_no_rows_and_more_dimensions(tvg, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [1, 20, 64, 300])
-def test_streams_graphs_and_repeats(tvg, rows, dtype):
+@pytest.mark.parametrize("rows,k", [(1, 256), (20, 256), (64, 256), (300, 256), (1100, 1100), (2100, 2060), (4100, 2600)])
+def test_streams_graphs_and_repeats(tvg, rows, k, dtype):
     """The same bits again, on another stream, with a workspace and an output of the caller's, over the residual, and from
     every replay of a graph whose adapter indices change in between."""
     import torch
-    p = make(rows, 1024, 256, 16, 8, dtype, rows, residual=True)
+    p = make(rows, 1024 if rows < 1000 else 192, k, 16, 8, dtype, rows, residual=True)
     call = lambda **kw: tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"], None, p["residual"], **kw)
     want = call()
     assert torch.equal(call(), want)
@@ -204,6 +219,16 @@ def test_streams_graphs_and_repeats(tvg, rows, dtype):
         assert torch.equal(y, eager), i
         assert i > 0 or bool((first < 0).any()) or torch.equal(y, want)
     p["adapter"].copy_(first)
+    # two calls at once, each with its own memory
+    other = dict(p, x=p["x"].flip(0).contiguous())
+    want2 = tvg.linear_lora_fused(other["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"], None, p["residual"])
+    torch.cuda.synchronize()
+    ys = []
+    for i in range(6):
+        with torch.cuda.stream(side if i % 2 else torch.cuda.current_stream()):
+            ys.append(tvg.linear_lora_fused((other if i % 2 else p)["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"], None, p["residual"]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want2 if i % 2 else want) for i, y in enumerate(ys))
     over = p["residual"].clone()
     p["residual"] = over
     assert call(out=over) is over
