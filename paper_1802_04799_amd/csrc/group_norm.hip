@@ -256,11 +256,8 @@ template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) 
             const int lo = max(g * a.cpg, first), hi = min((g + 1) * a.cpg, first + pass_width);
             const int base = (lo - first) / P, w = (hi - lo) / P;
             const int entries = w * t.rp, rows = t.row1 - t.row0;
-            const float inv_w = 1.0f / (float)w, inv_rp = 1.0f / (float)t.rp;
-            const auto rows_of = [&](int r) {              // rows of a lane: every rp-th
-                int rest;
-                return r < rows ? fast_div(rows - r + t.rp - 1, t.rp, inv_rp, &rest) : 0;
-            };
+            const float inv_w = 1.0f / (float)w;
+            const auto rows_of = [&](int r) { return r < rows ? (rows - r + t.rp - 1) / t.rp : 0; };       // every rp-th
             float s = 0.0f;
             for (int e = tl; e < entries; e += kTeam) {
                 int c;

@@ -209,6 +209,19 @@ def test_backward(tvg, shape, groups, act, dtype):
     check_backward(tvg, x, dy, groups, gamma, beta, act, dtype)
 
 
+# many row chunks, more of them than one round of loads joins, one chunk of many samples, more rows than lanes of odd channels
+LARGE = [((1, 300, 300, 64), 32), ((3, 112, 112, 64), 8), ((2, 190, 200, 36), 4), ((70, 60, 61, 24), 24), ((520, 100, 100, 16), 4),
+         ((1, 70000, 1), 1), ((1, 40000, 3), 3), ((1, 700, 5000), 8), ((1, 23, 5001), 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,groups", LARGE, ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v))
+def test_large_maps(tvg, shape, groups, dtype):
+    x, dy, gamma, beta = inputs(shape, dtype, sum(shape) + groups + 2)
+    check_forward(tvg, x, groups, gamma, beta, "silu", dtype)
+    check_backward(tvg, x, dy, groups, gamma, beta, "silu", dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_backward_of_relu_and_without_parameters(tvg, dtype):
     """x such that no z lies near zero, where a rounding would decide."""
@@ -272,9 +285,13 @@ def test_streams_graphs_and_repeats(tvg, dtype):
     room = torch.full((1 << 22,), 0xFF, dtype=torch.uint8, device="cuda")
     assert same(both(workspace=room))
     assert same(both(workspace=room[:0]))                     # too small: one of its own
-    with torch.cuda.stream(side):
-        both()
-    side.synchronize()
+    # two calls at once, each with its own memory
+    got = []
+    for i in range(6):
+        with torch.cuda.stream(side if i % 2 else torch.cuda.current_stream()):
+            got.append(both())
+    torch.cuda.synchronize()
+    assert all(same(g) for g in got)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         captured = both()
