@@ -203,6 +203,7 @@ template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) 
     int col;
     const int rp = fast_div(threadIdx.x, t.cols, 1.0f / (float)t.cols, &col);
     const T *x = static_cast<const T *>(a.x) + ((size_t)t.sample * a.p) * a.c + t.c0;
+    const int each = (t.row1 - t.row0) / t.rp, more = (t.row1 - t.row0) % t.rp;        // rows of a lane
     for (int g = threadIdx.x; g < ng; g += kThreads) group[3 * g] = group[3 * g + 1] = group[3 * g + 2] = 0.0f;
     for (int pass = 0; pass * t.cols * V < t.width; ++pass) {
         const int first = pass * t.cols * V, cc = first + col * V;        // channels of the pass, of this lane
@@ -257,7 +258,7 @@ template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) 
             const int base = (lo - first) / P, w = (hi - lo) / P;
             const int entries = w * t.rp, rows = t.row1 - t.row0;
             const float inv_w = 1.0f / (float)w;
-            const auto rows_of = [&](int r) { return r < rows ? (rows - r + t.rp - 1) / t.rp : 0; };       // every rp-th
+            const auto rows_of = [&](int r) { return each + (r < more); };     // (every rp-th)
             float s = 0.0f;
             for (int e = tl; e < entries; e += kTeam) {
                 int c;
