@@ -17,6 +17,8 @@
 // others do not; blocks of 16 tokens without it are skipped.  Nothing is multiplied by zero, so what an adapter holds
 // (infinities, NaN) reaches no other row, and a row's bits do not depend on the rows beside it.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "tvg_device.h"
 #include "tvg_internal.h"
@@ -723,6 +725,12 @@ template <typename T, int MB, int NB, bool WIDE> tvg_status launch_parts(LoraArg
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
+// f(0), f(1), ... as types, so that each is a constant
+template <typename F, int... I> __device__ __forceinline__ void for_constants(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+
 constexpr int kSlice = 64;                 // bytes of the reduction per step of the kernel below
 
 // Byte of a 16-byte piece (0..3) of a row's slice: two rows share 128 bytes, pieces permuted against bank conflicts.
@@ -932,15 +940,50 @@ template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __lau
         step(s + 1, xv[1], wv[1], xv[0], wv[0]);
     }
     const bool mixed = adapters > 0 && blocks == 0;
-    // the last slices, then, where all tokens have the same adapter, its blocks of ranks
+    constexpr bool kAhead = TM < 256;      // (the largest tile's registers have no room for two steps here)
+    // the last slices to fetch, then, where all tokens have the same adapter, its blocks of ranks
 #pragma unroll 1
-    for (const int end = turns + blocks; s < end; ++s) {
+    for (const int end = mixed ? turns : turns + blocks - (RING - 1); s < end; ++s) {
         behind();
         fetch_any(s + RING - 1);
-        read(s, xv[0], wv[0]);
-        wait_reads();                      // (the next step's barrier lets other waves write there)
-        multiply(xv[0], wv[0]);
+        if constexpr (kAhead) {
+            read(s + 1, xv[1], wv[1]);
+            multiply(xv[0], wv[0]);
+            wait_reads();                  // (the next step's barrier lets other waves write there)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) xv[0][n] = xv[1][n];
+#pragma unroll
+            for (int m = 0; m < MB; ++m) wv[0][m] = wv[1][m];
+        } else {
+            read(s, xv[0], wv[0]);
+            wait_reads();
+            multiply(xv[0], wv[0]);
+        }
     }
+    // what is in the ring (zeros where the sum has fewer steps than that)
+    if constexpr (!kAhead) {
+        if (!mixed) {
+            wait_loads<0>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+            for (const int end = s + RING - 1; s < end; ++s) {
+                read(s, xv[0], wv[0]);
+                multiply(xv[0], wv[0]);
+            }
+        }
+    } else if (!mixed)
+        for_constants([&](auto d) {
+            constexpr int kStep = decltype(d)::value;
+            if constexpr (kStep < RING - 2) {
+                wait_loads<(RING - 3 - kStep) * kLoads>();
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                read(s + kStep + 1, xv[(kStep + 1) & 1], wv[(kStep + 1) & 1]);
+            }
+            multiply(xv[kStep & 1], wv[kStep & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }, std::make_integer_sequence<int, RING - 1>());
     if (mixed) {
         int mine[NB], at = 0, j = 0;
 #pragma unroll
