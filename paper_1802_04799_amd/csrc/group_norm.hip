@@ -34,7 +34,12 @@ constexpr int kTeam = 16;                  // lanes that join the statistics of 
 // V elements of memory: 16 bytes or less.
 template <typename T, int V> struct Vec {
     typedef T type __attribute__((ext_vector_type(V)));
-    static __device__ __forceinline__ type load(const T *p) { return *reinterpret_cast<const type *>(p); }
+    // LAST: the memory is not read again; NT: not soon
+    template <bool LAST = false> static __device__ __forceinline__ type load(const T *p)
+    {
+        if constexpr (LAST) return __builtin_nontemporal_load(reinterpret_cast<const type *>(p));
+        else return *reinterpret_cast<const type *>(p);
+    }
     static __device__ __forceinline__ void get(const type &r, float *f)
     {
 #pragma unroll
@@ -43,7 +48,7 @@ template <typename T, int V> struct Vec {
             else f[i] = r[i];
         }
     }
-    static __device__ __forceinline__ void store(T *p, const float *f)
+    template <bool NT = false> static __device__ __forceinline__ void store(T *p, const float *f)
     {
         type r;
         if constexpr (sizeof(T) == 2 && V > 1) {
@@ -56,14 +61,15 @@ template <typename T, int V> struct Vec {
 #pragma unroll
             for (int i = 0; i < V; ++i) r[i] = f[i];
         }
-        *reinterpret_cast<type *>(p) = r;
+        if constexpr (NT) __builtin_nontemporal_store(r, reinterpret_cast<type *>(p));
+        else *reinterpret_cast<type *>(p) = r;
     }
 };
 template <typename T> struct Vec<T, 1> {
     typedef T type;
-    static __device__ __forceinline__ type load(const T *p) { return *p; }
+    template <bool LAST = false> static __device__ __forceinline__ type load(const T *p) { return *p; }
     static __device__ __forceinline__ void get(const type &r, float *f) { f[0] = Elem<T>::load(&r, 0); }
-    static __device__ __forceinline__ void store(T *p, const float *f) { Elem<T>::store(p, 0, f[0]); }
+    template <bool NT = false> static __device__ __forceinline__ void store(T *p, const float *f) { Elem<T>::store(p, 0, f[0]); }
 };
 
 template <typename T, int ACT> __device__ __forceinline__ float activate(float z)
@@ -96,6 +102,7 @@ struct NormArgs {
     int tiles;                             // n * blocks * chunks
     float eps;
     int act;
+    int passing;                           // two launches: more than the L2 caches hold; one: blocks of whole lines
 };
 
 // The part of the problem that a workgroup has.
@@ -325,7 +332,7 @@ __device__ __forceinline__ void join_chunks(const NormArgs &a, const Tile &t, in
     }
 }
 
-template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_apply_kernel(NormArgs a)
+template <typename T, int V, int ACT, bool WHOLE, bool PASS> __global__ __launch_bounds__(kThreads) void group_norm_apply_kernel(NormArgs a)
 {
     constexpr int U = 4;
     extern __shared__ float lds[];
@@ -346,7 +353,7 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
         const auto load = [&] {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (row + u * t.rp < t.row1) raw[u] = Vec<T, V>::load(x + (size_t)(row + u * t.rp) * a.c + cc);
+                if (row + u * t.rp < t.row1) raw[u] = Vec<T, V>::template load<PASS>(x + (size_t)(row + u * t.rp) * a.c + cc);
         };
         if (active) {
             load();
@@ -374,7 +381,7 @@ template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(k
                 Vec<T, V>::get(raw[u], f);
 #pragma unroll
                 for (int i = 0; i < V; ++i) f[i] = activate<T, ACT>(fmaf(f[i] - mean[i], mul[i], add[i]));
-                Vec<T, V>::store(y + (size_t)(row + u * t.rp) * a.c + cc, f);
+                Vec<T, V>::template store<true>(y + (size_t)(row + u * t.rp) * a.c + cc, f);
             }
         }
     }
@@ -531,7 +538,7 @@ __device__ __forceinline__ void reduce_channels(const NormArgs &a, int rows, int
 }
 
 // The first workgroups add up dgamma and dbeta, the others write dx.
-template <typename T, int V, int ACT, bool WHOLE>
+template <typename T, int V, int ACT, bool WHOLE, bool PASS>
 __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers)
 {
     constexpr int U = 4;
@@ -558,8 +565,8 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
             for (int u = 0; u < U; ++u)
                 if (row + u * t.rp < t.row1) {
                     const size_t at = (size_t)(row + u * t.rp) * a.c + cc;
-                    rx[u] = Vec<T, V>::load(x + at);
-                    rd[u] = Vec<T, V>::load(dy + at);
+                    rx[u] = Vec<T, V>::template load<PASS>(x + at);
+                    rd[u] = Vec<T, V>::template load<PASS>(dy + at);
                 }
         };
         Channels<V, WHOLE> k;
@@ -610,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
                     const float dz = activate_grad<T, ACT>(fd[i], fmaf(d, k.mul[i], k.add[i]));
                     fx[i] = fmaf(dz, k.mul[i], -fmaf(d, sb[i], sa[i]));
                 }
-                Vec<T, V>::store(dx + (size_t)(row + u * t.rp) * a.c + cc, fx);
+                Vec<T, V>::template store<true>(dx + (size_t)(row + u * t.rp) * a.c + cc, fx);
             }
         }
     }
@@ -721,7 +728,7 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
     __syncthreads();
     if (!active) return;
     for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) { mul[i] *= grstd[g]; });
-    const auto write = [&](auto act) {
+    const auto write_as = [&](auto act, auto pass) {
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
             const int row = lane_row + u * rp;
@@ -730,8 +737,12 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
             Vec<T, V>::get(raw[u], f);
 #pragma unroll
             for (int i = 0; i < V; ++i) f[i] = activate<T, decltype(act)::value>(fmaf(f[i] - mean[i], mul[i], add[i]));
-            Vec<T, V>::store(y + (size_t)row * a.c, f);
+            Vec<T, V>::template store<decltype(pass)::value>(y + (size_t)row * a.c, f);
         }
+    };
+    const auto write = [&](auto act) {
+        if (a.passing) write_as(act, std::true_type());
+        else write_as(act, std::false_type());
     };
     if (a.act == TVG_ACT_SILU) write(std::integral_constant<int, TVG_ACT_SILU>());
     else if (a.act == TVG_ACT_RELU) write(std::integral_constant<int, TVG_ACT_RELU>());
@@ -876,7 +887,7 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
         sa[i] = group[2 * g] * k.rstd[i];
         sb[i] = group[2 * g + 1] * (k.rstd[i] * k.rstd[i]);
     });
-    with_act([&](auto act) {
+    const auto write = [&](auto act, auto pass) {
         rows(act, [&](int u, float (&fx)[V], auto &&dz_of) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -884,8 +895,12 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
                 const float dz = dz_of(i, d);
                 fx[i] = fmaf(dz, k.mul[i], -fmaf(d, sb[i], sa[i]));
             }
-            Vec<T, V>::store(dx + (size_t)(lane_row + u * rp) * a.c, fx);
+            Vec<T, V>::template store<decltype(pass)::value>(dx + (size_t)(lane_row + u * rp) * a.c, fx);
         });
+    };
+    with_act([&](auto act) {
+        if (a.passing) write(act, std::true_type());
+        else write(act, std::false_type());
     });
 }
 
@@ -909,14 +924,23 @@ template <typename T, int V, bool WHOLE> tvg_status launch_grad_once(const NormA
 // Whether a lane's channels are always of one group.
 template <int V> bool whole_vectors(const NormArgs &a) { return a.cpg % V == 0; }
 
+template <typename T, int V, int ACT, bool WHOLE> void launch_apply(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
+{
+    if constexpr (V * sizeof(T) == 16)
+        if (a.passing) {
+            hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ACT, WHOLE, true>), dim3(a.tiles), dim3(kThreads), plan.lds_apply, stream, a);
+            return;
+        }
+    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ACT, WHOLE, false>), dim3(a.tiles), dim3(kThreads), plan.lds_apply, stream, a);
+}
+
 template <typename T, int V, bool WHOLE> tvg_status launch_forward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
 {
     if (plan.once) return launch_once<T, V, WHOLE>(a, plan, stream);
-    const dim3 grid(a.tiles), threads(kThreads);
-    hipLaunchKernelGGL((group_norm_stats_kernel<T, V, WHOLE>), grid, threads, plan.lds_stats, stream, a);
-    if (a.act == TVG_ACT_SILU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_SILU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
-    else if (a.act == TVG_ACT_RELU) hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_RELU, WHOLE>), grid, threads, plan.lds_apply, stream, a);
-    else hipLaunchKernelGGL((group_norm_apply_kernel<T, V, TVG_ACT_NONE, WHOLE>), grid, threads, plan.lds_apply, stream, a);
+    hipLaunchKernelGGL((group_norm_stats_kernel<T, V, WHOLE>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
+    if (a.act == TVG_ACT_SILU) launch_apply<T, V, TVG_ACT_SILU, WHOLE>(a, plan, stream);
+    else if (a.act == TVG_ACT_RELU) launch_apply<T, V, TVG_ACT_RELU, WHOLE>(a, plan, stream);
+    else launch_apply<T, V, TVG_ACT_NONE, WHOLE>(a, plan, stream);
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 template <typename T, int V> tvg_status launch_forward(const NormArgs &a, const NormPlan &plan, hipStream_t stream)
@@ -928,7 +952,12 @@ template <typename T, int V, int ACT, bool WHOLE> tvg_status launch_grad(const N
 {
     const int reducers = a.dgamma || a.dbeta ? (a.c + kReduceChannels - 1) / kReduceChannels : 0;
     hipLaunchKernelGGL((group_norm_grad_sums_kernel<T, V, ACT, WHOLE>), dim3(a.tiles), dim3(kThreads), plan.lds_stats, stream, a);
-    hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a, reducers);
+    if constexpr (V * sizeof(T) == 16)
+        if (a.passing) {
+            hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE, true>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a, reducers);
+            return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
+        }
+    hipLaunchKernelGGL((group_norm_grad_apply_kernel<T, V, ACT, WHOLE, false>), dim3(a.tiles + reducers), dim3(kThreads), plan.lds_apply, stream, a, reducers);
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
@@ -965,6 +994,16 @@ int vector_width(const NormProblem &p, std::initializer_list<const void *> point
     return v;
 }
 
+// Results that pass the caches by leave them to x.  64 maps 112x112x256: 261 us, stores that do 242, loads of the second launch too
+// 224 (backward 417, 398, 368); 8 maps 64x64x320, which the L2 caches (32 MB) keep, 24.5, 23.5, 24.4.  Of one launch's blocks only
+// whole lines do: 64 maps 28x28x512 in blocks of 256 bytes 29.3 us and 27.1, 64 maps 56x56x256 in blocks of 80 bytes 65 and 115.
+bool passing(const NormProblem &p, const NormPlan &plan)
+{
+    const int64_t size = p.dtype == TVG_BF16 ? 2 : 4;
+    if (plan.once) return plan.block * size % 128 == 0 && p.c * size % 128 == 0;
+    return (int64_t)p.n * p.p * p.c * size > (32 << 20);
+}
+
 NormArgs make_args(const NormProblem &p, const NormPlan &plan)
 {
     NormArgs a{};
@@ -973,6 +1012,7 @@ NormArgs make_args(const NormProblem &p, const NormPlan &plan)
     a.tiles = p.n * plan.blocks * plan.chunks;
     a.eps = p.eps;
     a.act = p.act;
+    a.passing = passing(p, plan);
     return a;
 }
 
