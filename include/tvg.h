@@ -287,9 +287,9 @@ typedef enum { TVG_ACT_NONE = 0, TVG_ACT_RELU = 1, TVG_ACT_SILU = 2 } tvg_activa
  * flags must be 0.  Any alignment of whole elements (fp32 ones 4 bytes); 16 bytes and c a multiple of 8 (bf16) or 4 (fp32)
  * are the fast way.
  * Errors: TVG_ERR_BAD_SHAPE for extents below 1, c no multiple of groups, eps negative or not finite; TVG_ERR_UNSUPPORTED for
- * unknown dtype, activation or flags, 2^31 elements, 2^30 pixels, n of 2^18
- * or c of 2^20 or more; TVG_ERR_WORKSPACE for a
- * workspace that is NULL, short or not 256-byte aligned (where the query says more than 0 bytes).
+ * unknown dtype, activation or flags, 2^31 elements, 2^30 pixels, n of 2^18 or c of 2^20 or more; TVG_ERR_WORKSPACE for a
+ * workspace that is NULL, short or not 256-byte aligned (where the query says more than 0 bytes).  A workspace is scratch of one
+ * call at a time: calls that may overlap, on two streams or in two graphs, take one each.
  */
 typedef struct {
     int32_t n, pixels, c, groups;

@@ -6,9 +6,12 @@
 //   dbeta = sum_n S1, dgamma = sum_n S2, dx = rstd (gamma dz - (a + xhat b) / m)
 //   with a, b the sums of gamma S1, gamma S2 over a group's channels and m its elements
 //
-// Bound by memory: about 10 (forward) or 25 (backward) operations an element.  Two launches: the first leaves partial
-// statistics of row chunks in the workspace, the second joins those of its sample in a fixed order and applies them, the last
-// chunk first: it is the one whose rows the caches still hold.
+// Bound by memory: about 10 (forward) or 25 (backward) operations an element.  Where a block of channels of a sample fits a
+// workgroup's registers one launch reads it once (32 maps 56x56x256 in bf16, 51 MB: 29 us, 3.6 TB/s of a copy's 5.1).  Else two
+// launches: the first leaves partial statistics of row chunks in the workspace, the second joins those of its sample in a fixed
+// order and applies them, the last chunk first: it is the one whose rows the caches still hold (64 maps 112x112x256, 411 MB: 74 us
+// and 149, 5.5 TB/s over both reads and the write; backward 147 us and 219, 5.6 TB/s over four reads and a write).
+// Values are rounded to fewer bits once, as y or dx; statistics, sums, gamma, beta and their gradients are fp32.
 //
 // A workgroup covers a chunk of rows of one sample and a block of whole groups; a lane covers V adjacent channels (16
 // bytes where the channels allow it) of every RP-th row, so that what it needs of a channel stays in registers and groups
@@ -102,7 +105,7 @@ struct NormArgs {
     int tiles;                             // n * blocks * chunks
     float eps;
     int act;
-    int passing;                           // two launches: more than the L2 caches hold; one: blocks of whole lines
+    int passing;                           // results pass the caches by, and so does x when it is read last
 };
 
 // The part of the problem that a workgroup has.
@@ -199,7 +202,8 @@ __device__ __forceinline__ void join_rows(const typename Vec<T, V>::type (&raw)[
     }
 }
 
-// LDS: per channel of a pass the lanes' (mean, M2, rows), then per group (elements, mean, M2).
+// Statistics of a chunk.  LDS: per entry of a pass the lanes' mean and M2, then per group (elements, mean, M2).  Eight rows in
+// flight a lane: 64 maps 112x112x256 74 us, 5.5 TB/s with what the caches hold of a call before.
 template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_stats_kernel(NormArgs a)
 {
     constexpr int U = 8, Q = WHOLE ? 1 : V;                // entries per lane
@@ -332,6 +336,8 @@ __device__ __forceinline__ void join_chunks(const NormArgs &a, const Tile &t, in
     }
 }
 
+// y from the statistics of all chunks, which every workgroup joins for its own groups (a launch between would cost 4 us).
+// 64 maps 112x112x256: 149 us, 822 MB at 5.5 TB/s.
 template <typename T, int V, int ACT, bool WHOLE, bool PASS> __global__ __launch_bounds__(kThreads) void group_norm_apply_kernel(NormArgs a)
 {
     constexpr int U = 4;
@@ -410,6 +416,7 @@ template <int V, bool WHOLE> struct Channels {
     }
 };
 
+// S1 and S2 of a chunk's rows per channel, and gamma's sums of them per group.  64 maps 112x112x256: 147 us, 822 MB at 5.6 TB/s.
 template <typename T, int V, int ACT, bool WHOLE> __global__ __launch_bounds__(kThreads) void group_norm_grad_sums_kernel(NormArgs a)
 {
     constexpr int U = 4;
@@ -537,7 +544,8 @@ __device__ __forceinline__ void reduce_channels(const NormArgs &a, int rows, int
     }
 }
 
-// The first workgroups add up dgamma and dbeta, the others write dx.
+// The first workgroups add up dgamma and dbeta, the others write dx: z and its derivative again from x, cheaper than a stored dz.
+// 64 maps 112x112x256: 219 us, 1233 MB at 5.6 TB/s.
 template <typename T, int V, int ACT, bool WHOLE, bool PASS>
 __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArgs a, int reducers)
 {
@@ -625,7 +633,8 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
 
 // ---------------------------------------------------------------------------------------
 // One launch, where a sample's block of channels fits the registers of a workgroup: NV vectors a lane, read once.
-// Mean first, then the squared distances from it, both over the workgroup's LDS.
+// Mean first, then the squared distances from it, both over the workgroup's LDS.  Bound by latency where it is small (one map
+// 7x7x512 5.3 us: a launch, a read, two sums over LDS), by reading and writing in turn where it is large (51 MB 29 us).
 // ---------------------------------------------------------------------------------------
 
 // Sums over the channels and lanes of every group, given a value per channel and lane in LDS ([rp][width]); f(group, sum) by
@@ -762,7 +771,7 @@ template <typename T, int V, bool WHOLE> tvg_status launch_once(const NormArgs &
 }
 
 // The same for the backward pass: x and dy in registers.  The sums of a sample's channels go to the workspace ([n][c][2]), or,
-// of the only sample, to dgamma and dbeta.
+// of the only sample, to dgamma and dbeta.  2 maps 14x14x256 in fp32: 6.7 us and 1.6 of the launch that adds up the samples.
 constexpr int kSumParts = 16;
 template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launch_bounds__(THREADS) void group_norm_grad_once_kernel(NormArgs a)
 {
@@ -1019,7 +1028,8 @@ NormArgs make_args(const NormProblem &p, const NormPlan &plan)
 }  // namespace
 
 // The plan of one launch, if a block of channels fits a workgroup's registers: blocks for a workgroup a CU, 64 bytes of a row
-// at least where that fits, 32 at least.
+// at least where that fits, 32 at least.  Two launches took 16.8 us for one map 7x7x512 where one takes 5.3, and 50 us for 32 maps
+// 56x56x256 where one takes 29; gradients of 2 maps 14x14x256 (fp32) 10.1 and 9.5.
 static bool plan_once(const NormProblem &p, int vector, bool backward, NormPlan *plan)
 {
     const int cpg = p.c / p.groups, size = p.dtype == TVG_BF16 ? 2 : 4;
@@ -1035,8 +1045,10 @@ static bool plan_once(const NormProblem &p, int vector, bool backward, NormPlan 
     units = std::min<int64_t>(units, p.c / unit);
     while (units > 1 && !fits((int)units * unit, 2)) --units;
     const int width = (int)units * unit;
-    // (few workgroups with much each: the two launches spread it)
-    if ((int64_t)p.n * ((p.c + width - 1) / width) < kComputeUnits / 2 && (int64_t)p.p * width * size > (backward ? 16 : 32) * 1024) return false;
+    // Few workgroups with much each: the two launches spread it.  One launch and two, us: 4 maps 28x28x256 (50 KB a workgroup) 8.6
+    // and 11.6, one map 40x40x512 (100 KB) 13.7 and 13.2, one map 56x56x256 (200 KB) 17.8 and 13.2; gradients of one map 20x20x512
+    // (25 KB) 9.7 and 13.3, of 4 maps 28x28x256 15.8 and 13.8.
+    if ((int64_t)p.n * ((p.c + width - 1) / width) < kComputeUnits / 2 && (int64_t)p.p * width * size > (backward ? 32 : 64) * 1024) return false;
     if (!fits(width, 2) || (width * size < (backward ? 64 : 32) && width < p.c)) return false;
     int k = 0;
     while (!fits(width, k)) ++k;

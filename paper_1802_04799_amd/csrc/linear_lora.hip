@@ -2,7 +2,10 @@
 //   y = act(x W^T + bias + scale_i (x A_i^T) B_i^T + residual),  i = adapter[row]
 //
 // Two launches.  The first makes the adapters' middle vectors h = scale_i A_i x.  The second is a matrix product whose
-// reduction goes on, after the c channels, over the rank: the same accumulators take B_i h.
+// reduction goes on, after the c channels, over the rank: the same accumulators take B_i h.  With few tiles the first launch makes
+// h and the product in parts of the reduction, the second adds both up.  Many rows are bound by the matrix cores and what feeds
+// them (8192 rows 4096 -> 4096 in bf16: 25 us for h, 207 for the product, 1.33 PFLOP/s), few by the weights' bytes and the two
+// launches (64 rows 4096 -> 4096: 10.9 and 3.0 us for 34 MB).
 //
 // Both types are the same kernels in bytes: a lane's operand of a 16x16 tile is 16 bytes, 8 bf16 of one
 // v_mfma_f32_16x16x32_bf16 or 4 fp32 of four v_mfma_f32_16x16x4_f32, whose order of the reduction is that of the loads.
@@ -285,7 +288,8 @@ template <int N> __device__ __forceinline__ int distinct_adapters(const int (&mi
 }
 
 // h of NB blocks of 16 tokens and JB blocks of 16 ranks; the waves take 128 bytes of the reduction in turn and add up through
-// LDS.  Adapters of the tile: every slots-th of them.
+// LDS.  Adapters of the tile: every slots-th of them.  Bound by reading x, once per adapter of the tile: 8192 rows of 4096 (67 MB)
+// with 16 adapters of rank 32 25 us, 2.7 TB/s.  h leaves in bf16 as two numbers, whose sum has an error of 2^-17.
 template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __forceinline__ void shrink_tile(const LoraArgs &a, int b, unsigned char *lds)
 {
     constexpr int kPart = kPartBytes<T, JB, NB, W, WIDE, KB>;
@@ -338,7 +342,8 @@ template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __for
 }
 
 // The rows in the order of their adapters (modulo kBins, rows without one last), for a product whose tiles then have few
-// adapters each.  The order of rows of an adapter is left to chance: a row's result does not depend on its place.
+// adapters each: 1200 rows of 150 requests with 24 adapters of rank 64, 2048 -> 8192, took 148 us in their own order and 97 in
+// this one.  The order of rows of an adapter is left to chance: a row's result does not depend on its place.
 constexpr int kBins = 2048, kBinsPerLane = 5;
 
 // bins[bin] += 1 for every lane with `ok`; what it was before, every lane one more than the last.  Lanes of a run add up first:
@@ -622,12 +627,13 @@ template <typename T> __device__ __forceinline__ void store4(const LoraArgs &a, 
 }
 
 // A workgroup has 16 NB tokens x 16 MB channels and its waves split the reduction, without a barrier; then they take the
-// adapters' blocks of ranks in turn, and add up through LDS.  PARTS: the product is there already, in parts of the reduction.
-enum { kAnyRows = 0, kWideRows = 1, kParts = 2 };
+// adapters' blocks of ranks in turn, and add up through LDS.  kParts: the product is there already, in parts of the reduction, whose
+// reading is all of it (64 rows 4096 -> 4096: 3.0 us alone, 5.2 with adapters).  kAnyRows: rows at any element, operands straight from
+// memory, 30 GB/s a CU (1200 rows 2001 -> 2000 in bf16 155 us, where 2000 -> 2000 takes 28 through LDS; fp32 168 and 108).
+enum { kAnyRows = 0, kParts = 2 };
 template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bounds__(64 * W, 2) void linear_lora_waves_kernel(LoraArgs a)
 {
-    constexpr int kPart = MODE == kWideRows ? kPartBytes<T, MB, NB, W, true, kAllLds> : MB * NB * 1024;
-    static_assert(kPart >= NB * MB * 1024, "the sums lie where the chunks were");
+    constexpr int kPart = MB * NB * 1024;
     extern __shared__ __align__(16) unsigned char lds[];
     const int tile = xcd_remap(blockIdx.x, a.tiles);
     const int tm = tile / a.tiles_n, tn = tile - tm * a.tiles_n;
@@ -649,7 +655,7 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
                         acc[m][n] += *reinterpret_cast<const float4v *>(a.parts + ((size_t)s * a.rows + row) * a.parts_row + ch0 + m * 16 + quad * 4);
                 }
     } else {
-        wave_product<T, MB, NB, W, MODE == kWideRows, kAllLds>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
+        wave_product<T, MB, NB, W, false, kAllLds>(static_cast<const T *>(a.x) + (size_t)row0 * a.c, a.rows - row0,
                                                       static_cast<const T *>(a.w) + (size_t)ch0 * a.c, a.k - ch0, a.c, wave,
                                                       (a.c + 8 * kPer16<T> - 1) / (8 * kPer16<T>), part, lane, acc);
     }
@@ -661,7 +667,8 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
 }
 
 // Few rows: the first workgroups make h, the others parts of the product, 16 NB tokens x 16 MB channels over a part of the
-// reduction, which the next launch adds up.
+// reduction, which the next launch adds up.  64 rows 4096 -> 4096 in bf16: 10.9 us for the weights' 34 MB (3.1 TB/s; 12.7 with h of 32
+// adapters), where the library's product takes 19; one row 1024 -> 1024 4.2 us, a launch's latency.
 template <typename T, int MB, int NB, bool WIDE> __global__ __launch_bounds__(64 * product_waves(MB, NB), 2) void lora_parts_kernel(LoraArgs a)
 {
     constexpr int W = product_waves(MB, NB), kPart = kPartBytes<T, MB, NB, W, WIDE, kAllLds>;
@@ -702,7 +709,7 @@ template <typename K> bool allow_lds(K kernel, size_t bytes)
 template <typename T, int MB, int NB, int W, int MODE> tvg_status launch_waves(LoraArgs a, hipStream_t stream)
 {
     const auto kernel = linear_lora_waves_kernel<T, MB, NB, W, MODE>;
-    constexpr size_t kLds = (size_t)W * (MODE == kWideRows ? kPartBytes<T, MB, NB, W, true, kAllLds> : MB * NB * 1024);
+    constexpr size_t kLds = (size_t)W * MB * NB * 1024;
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     a.tiles_n = (a.k + 16 * MB - 1) / (16 * MB);
@@ -742,7 +749,9 @@ __device__ __forceinline__ int slice_at(int row, int piece)
 
 // Rows of whole 16-byte pieces: TM tokens x TN channels, WR x WC waves.  Both operands' slices come straight from memory
 // into a ring of RING steps in LDS, RING - 1 steps ahead; a wave reads the operands of the next step while it multiplies those
-// of this one, with one barrier a step.
+// of this one, with one barrier a step.  Clocks a step, of which the matrix instructions take: 256 x 256 bf16 1360 and 1024 (two
+// waves a SIMD, all of whose registers it takes), 64 x 64 bf16 260 and 64 (what comes from the caches bounds it: 8 KB a step), 64 x 64
+// fp32 690 and 512.  Beside the steps: 2 us until the first slices are there, 1 to 5 us of stores, which all tiles do together.
 template <typename T, int TM, int TN, int WR, int WC, int RING> __global__ __launch_bounds__(64 * WR * WC, 2) void linear_lora_tile_kernel(LoraArgs a)
 {
     constexpr int W = WR * WC, kLoads = (TM + TN) / 16 / W, kLoadsX = TM / 16 / W;
