@@ -626,10 +626,23 @@ template <typename T> __device__ __forceinline__ void store4(const LoraArgs &a, 
         }
 }
 
+// Rows of x, w and a of c elements, behind each other as rows of `pieces` 16 bytes, zeros behind the last element: a copy, 13 us
+// for 1200 rows of 2001 and 2000 of w (bf16, launch included).
+template <typename T> __global__ __launch_bounds__(256) void lora_pack_kernel(LoraArgs a, uint32_t rows, uint32_t pieces, T *to)
+{
+    const uint32_t at = blockIdx.x * 256u + threadIdx.x, row = at / pieces, piece = at - row * pieces;
+    if (row >= rows) return;
+    const uint32_t xw = (uint32_t)a.rows + a.k;
+    const T *from = row < (uint32_t)a.rows ? static_cast<const T *>(a.x) + (size_t)row * a.c
+                    : row < xw             ? static_cast<const T *>(a.w) + (size_t)(row - a.rows) * a.c
+                                           : static_cast<const T *>(a.a) + (size_t)(row - xw) * a.c;
+    *reinterpret_cast<uint4v *>(to + (size_t)at * kPer16<T>) = load16(from, (int)piece * kPer16<T>, a.c);
+}
+
 // A workgroup has 16 NB tokens x 16 MB channels and its waves split the reduction, without a barrier; then they take the
 // adapters' blocks of ranks in turn, and add up through LDS.  kParts: the product is there already, in parts of the reduction, whose
 // reading is all of it (64 rows 4096 -> 4096: 3.0 us alone, 5.2 with adapters).  kAnyRows: rows at any element, operands straight from
-// memory, 30 GB/s a CU (1200 rows 2001 -> 2000 in bf16 155 us, where 2000 -> 2000 takes 28 through LDS; fp32 168 and 108).
+// memory, 30 GB/s a CU (1200 rows 2001 -> 2000 in bf16 155 us): left for tensors that begin between 16-byte pieces and for short rows.
 enum { kAnyRows = 0, kParts = 2 };
 template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bounds__(64 * W, 2) void linear_lora_waves_kernel(LoraArgs a)
 {
@@ -1119,8 +1132,38 @@ int ring_tile(const LoraProblem &p)
     return (int64_t)95 * rounds(t256) * kComputeUnits <= (int64_t)44 * std::max(t128, kComputeUnits) ? 256 : 128;
 }
 
-template <typename T> tvg_status launch(const LoraProblem &p, LoraArgs &a, hipStream_t stream)
+// Rows that are no whole 16-byte pieces are copied to rows that are, where a round of 64 x 64 tiles reads each often enough and a
+// row is no shorter than two pieces of 128 bytes.  Copied and read as they are, us: 8192 rows 4097 -> 4096 in bf16 314 and 3168 (fp32
+// 1997 and 3260), 1200 rows 2001 -> 2000 49 and 171 (132 and 181), 1200 rows 133 -> 2000 19 and 24 (33 and 34), 1000 rows
+// 131 -> 1040, the smallest copied, 17 and 15 (24 and 20).
+size_t elem_size(const LoraProblem &p) { return p.dtype == TVG_BF16 ? 2 : 4; }
+int packed_c(const LoraProblem &p)
 {
+    const int e = 16 / (int)elem_size(p);
+    return (p.c + e - 1) / e * e;
+}
+bool packs(const LoraProblem &p)
+{
+    return packed_c(p) != p.c && p.c * elem_size(p) >= 256 && packed_c(p) * elem_size(p) < 1 << 23 && tiles_of(p, 64, 64) >= kComputeUnits;
+}
+size_t packed_rows(const LoraProblem &p) { return (size_t)p.rows + p.k + (size_t)p.adapters * p.rank; }
+size_t packed_at(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+template <typename T> tvg_status launch(const LoraProblem &problem, LoraArgs &a, hipStream_t stream)
+{
+    LoraProblem p = problem;
+    if (packs(p)) {
+        const size_t rows = packed_rows(p);
+        const uint32_t pieces = (uint32_t)(packed_c(p) / kPer16<T>);
+        T *to = reinterpret_cast<T *>(a.h + packed_at(plan_parts(p, false).bytes));
+        hipLaunchKernelGGL((lora_pack_kernel<T>), dim3((unsigned)((rows * pieces + 255) / 256)), dim3(256), 0, stream, a, (uint32_t)rows, pieces, to);
+        if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
+        p.c = a.c = packed_c(p);
+        a.x = to;
+        a.w = to + (size_t)p.rows * p.c;
+        a.a = to + ((size_t)p.rows + p.k) * p.c;
+        a.wide_rows = 1;
+    }
     const bool wide = a.wide_rows && (size_t)p.c * sizeof(T) < 1 << 23;
     const PartsPlan parts = plan_parts(p, wide);
     if (parts.use) return launch_few_tiles<T>(parts, wide, a, stream);
@@ -1145,7 +1188,9 @@ template <typename T> tvg_status launch(const LoraProblem &p, LoraArgs &a, hipSt
 
 size_t linear_lora_workspace(const LoraProblem &p)
 {
-    return p.rows == 0 ? 0 : std::max(plan_parts(p, true).bytes, plan_parts(p, false).bytes);
+    if (p.rows == 0) return 0;
+    const size_t bytes = std::max(plan_parts(p, true).bytes, plan_parts(p, false).bytes);
+    return packs(p) ? packed_at(bytes) + packed_rows(p) * packed_c(p) * elem_size(p) : bytes;
 }
 
 tvg_status launch_linear_lora(const LoraProblem &p, const LoraPointers &ptr, hipStream_t stream)

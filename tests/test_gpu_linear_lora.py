@@ -97,6 +97,32 @@ def test_large_projection(tvg, rows, c, k, rank, adapters, dtype):
     check(tvg, make(rows, c, k, rank, adapters, dtype, seed, residual=True, bias=True, scale=False), ("relu", "silu")[seed % 2], dtype)
 
 
+# ... of many tiles whose rows are no whole 16-byte pieces
+RAGGED = [(1100, 133, 1100, 16, 5), (2100, 515, 2060, 12, 9), (300, 1001, 6001, 20, 2), (4100, 250, 2601, 16, 30), (1100, 129, 1100, 5, 300)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,k,rank,adapters", RAGGED)
+def test_large_projection_of_ragged_rows(tvg, rows, c, k, rank, adapters, dtype):
+    import torch
+    seed = rows + c + k + rank
+    p = make(rows, c, k, rank, adapters, dtype, seed, residual=True, bias=True)
+    check(tvg, p, ("relu", "silu")[seed % 2], dtype)
+    # without adapters: the same product
+    y = tvg.linear_lora_fused(p["x"], p["w"], None, None, None)
+    none = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    assert torch.equal(y, tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], none))
+    # an adapter of infinities, rows of NaN: the others keep their bits
+    want = tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"], p["bias"], p["residual"])
+    a, x = p["a"].clone(), p["x"].clone()
+    a[0] = float("inf")
+    x[1] = float("nan")
+    got = tvg.linear_lora_fused(x, p["w"], a, p["b"], p["adapter"], p["scale"], p["bias"], p["residual"])
+    keep = p["adapter"] != 0
+    keep[1] = False
+    assert bool(torch.isnan(got[1]).all()) and torch.equal(got[keep], want[keep])
+
+
 def assignments(rows, adapters):
     """Rows of requests of many kinds: one adapter, none, long runs, single rows, unsorted, indices out of range."""
     import torch
