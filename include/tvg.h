@@ -321,7 +321,7 @@ tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const 
  * added in a fixed order.
  * rows == 0 is TVG_OK and launches nothing.  adapters == 0 is a plain projection: a, b, adapter and scale are ignored.
  * flags must be 0.  Any alignment of whole elements; the fast way is 16-byte alignment of x, w, a and y, c and k multiples of 8
- * (bf16) or 4 (fp32).
+ * (bf16) or 4 (fp32).  For other c the workspace may hold copies of x, w and a with longer rows, made by every call.
  * Errors: TVG_ERR_BAD_SHAPE for c, k or rank below 1, rows or adapters below 0; TVG_ERR_UNSUPPORTED for unknown dtype,
  * activation or flags, rank above 256, rows, c or k of 2^24 or more and tensors of 2^31 elements or more; TVG_ERR_WORKSPACE as above.
  */

@@ -1135,7 +1135,10 @@ int ring_tile(const LoraProblem &p)
 // Rows that are no whole 16-byte pieces are copied to rows that are, where a round of 64 x 64 tiles reads each often enough and a
 // row is no shorter than two pieces of 128 bytes.  Copied and read as they are, us: 8192 rows 4097 -> 4096 in bf16 314 and 3168 (fp32
 // 1997 and 3260), 1200 rows 2001 -> 2000 49 and 171 (132 and 181), 1200 rows 133 -> 2000 19 and 24 (33 and 34), 1000 rows
-// 131 -> 1040, the smallest copied, 17 and 15 (24 and 20).
+// 131 -> 1040, the smallest copied, 17 and 15 (24 and 20).  With fewer tiles where that is as much work as 16 rows 4096 -> 4096, and
+// in bf16: 16 rows 4097 -> 4096 28 and 34, 64 rows 29 and 82, 777 rows 1001 -> 515 18 and 28, 64 rows 1001 -> 1024 13 and 12; fp32, whose
+// products take longer, 100 rows 4097 -> 4096 98 and 77, 777 rows 1001 -> 515 36 and 32.  Not where the adapters, of which a call
+// may use a few, would be most of the copy.
 size_t elem_size(const LoraProblem &p) { return p.dtype == TVG_BF16 ? 2 : 4; }
 int packed_c(const LoraProblem &p)
 {
@@ -1144,10 +1147,18 @@ int packed_c(const LoraProblem &p)
 }
 bool packs(const LoraProblem &p)
 {
-    return packed_c(p) != p.c && p.c * elem_size(p) >= 256 && packed_c(p) * elem_size(p) < 1 << 23 && tiles_of(p, 64, 64) >= kComputeUnits;
+    return packed_c(p) != p.c && p.c * elem_size(p) >= 256 && packed_c(p) * elem_size(p) < 1 << 23 &&
+           (int64_t)p.adapters * p.rank <= (int64_t)p.rows + p.k &&
+           (tiles_of(p, 64, 64) >= kComputeUnits || (p.dtype == TVG_BF16 && (double)p.rows * p.c * p.k >= 1 << 28));
+}
+// Workspace in front of the copies.
+size_t front_bytes(const LoraProblem &p)
+{
+    LoraProblem q = p;
+    q.c = packed_c(p);
+    return (std::max(std::max(plan_parts(p, true).bytes, plan_parts(p, false).bytes), plan_parts(q, true).bytes) + 255) & ~(size_t)255;
 }
 size_t packed_rows(const LoraProblem &p) { return (size_t)p.rows + p.k + (size_t)p.adapters * p.rank; }
-size_t packed_at(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 template <typename T> tvg_status launch(const LoraProblem &problem, LoraArgs &a, hipStream_t stream)
 {
@@ -1155,7 +1166,7 @@ template <typename T> tvg_status launch(const LoraProblem &problem, LoraArgs &a,
     if (packs(p)) {
         const size_t rows = packed_rows(p);
         const uint32_t pieces = (uint32_t)(packed_c(p) / kPer16<T>);
-        T *to = reinterpret_cast<T *>(a.h + packed_at(plan_parts(p, false).bytes));
+        T *to = reinterpret_cast<T *>(a.h + front_bytes(p));
         hipLaunchKernelGGL((lora_pack_kernel<T>), dim3((unsigned)((rows * pieces + 255) / 256)), dim3(256), 0, stream, a, (uint32_t)rows, pieces, to);
         if (hipGetLastError() != hipSuccess) return TVG_ERR_LAUNCH;
         p.c = a.c = packed_c(p);
@@ -1189,8 +1200,7 @@ template <typename T> tvg_status launch(const LoraProblem &problem, LoraArgs &a,
 size_t linear_lora_workspace(const LoraProblem &p)
 {
     if (p.rows == 0) return 0;
-    const size_t bytes = std::max(plan_parts(p, true).bytes, plan_parts(p, false).bytes);
-    return packs(p) ? packed_at(bytes) + packed_rows(p) * packed_c(p) * elem_size(p) : bytes;
+    return packs(p) ? front_bytes(p) + packed_rows(p) * packed_c(p) * elem_size(p) : std::max(plan_parts(p, true).bytes, plan_parts(p, false).bytes);
 }
 
 tvg_status launch_linear_lora(const LoraProblem &p, const LoraPointers &ptr, hipStream_t stream)

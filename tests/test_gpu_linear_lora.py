@@ -98,7 +98,7 @@ def test_large_projection(tvg, rows, c, k, rank, adapters, dtype):
 
 
 # ... of many tiles whose rows are no whole 16-byte pieces
-RAGGED = [(1100, 133, 1100, 16, 5), (2100, 515, 2060, 12, 9), (300, 1001, 6001, 20, 2), (4100, 250, 2601, 16, 30), (1100, 129, 1100, 5, 300)]
+RAGGED = [(1100, 133, 1100, 16, 5), (2100, 515, 2060, 12, 9), (300, 1001, 6001, 20, 2), (4100, 250, 2601, 16, 30), (1100, 129, 1100, 5, 300), (1100, 133, 1100, 16, 200)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -114,6 +114,30 @@ def test_large_projection_of_ragged_rows(tvg, rows, c, k, rank, adapters, dtype)
     assert torch.equal(y, tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], none))
     # an adapter of infinities, rows of NaN: the others keep their bits
     want = tvg.linear_lora_fused(p["x"], p["w"], p["a"], p["b"], p["adapter"], p["scale"], p["bias"], p["residual"])
+    a, x = p["a"].clone(), p["x"].clone()
+    a[0] = float("inf")
+    x[1] = float("nan")
+    got = tvg.linear_lora_fused(x, p["w"], a, p["b"], p["adapter"], p["scale"], p["bias"], p["residual"])
+    keep = p["adapter"] != 0
+    keep[1] = False
+    assert bool(torch.isnan(got[1]).all()) and torch.equal(got[keep], want[keep])
+
+
+# ... of few tiles.  (Their product is cut into parts by what h leaves of the CUs, so that a call without adapters may add up in
+# another order: within the tolerance, not bit by bit.)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,k,rank,adapters", [(40, 4097, 1700, 16, 5), (777, 1001, 515, 12, 6), (17, 4099, 4096, 20, 20), (2, 20001, 7000, 16, 2)])
+def test_few_tiles_of_ragged_rows(tvg, rows, c, k, rank, adapters, dtype):
+    import torch
+    seed = rows + c + k + rank
+    p = make(rows, c, k, rank, adapters, dtype, seed, residual=True, bias=True)
+    want = check(tvg, p, None, dtype)
+    none = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    bare = dict(p, adapter=none, bias=None, residual=None)
+    check(tvg, bare, None, dtype)
+    y = tvg.linear_lora_fused(p["x"], p["w"], None, None, None)
+    y64, tol = wanted(bare, None, dtype)
+    assert bool(((y.double() - y64).abs() <= tol).all())
     a, x = p["a"].clone(), p["x"].clone()
     a[0] = float("inf")
     x[1] = float("nan")
