@@ -556,21 +556,24 @@ __device__ __forceinline__ void store_rows(const LoraArgs &a, int channel0, cons
 }
 
 // The adapters' part of 16 MB channels x 16 NB tokens (16 NB <= 64), operands straight from memory, those of the next block of
-// ranks under way while this one's are multiplied.  Of the blocks of all adapters the wave takes every W-th.
-// mine: the adapter of token row0 + lane, -1 for none.
+// ranks under way while this one's are multiplied.  Of the blocks of all adapters the wave takes every W-th (W a power of two).
+// mine: the adapter of token row0 + lane, -1 for none; start: the wave that takes the first block of that adapter.  Returns
+// whether this wave took any.
 template <typename T, int MB, int NB, int W>
-__device__ __forceinline__ void add_adapters(const LoraArgs &a, int mine, int channel0, int row0, int lane, int wave, float4v (&acc)[MB][NB])
+__device__ __forceinline__ bool add_adapters(const LoraArgs &a, int mine, int channel0, int row0, int lane, int wave, int &start, float4v (&acc)[MB][NB])
 {
     const int rsel = lane & 15, quad = lane >> 4;
     uint64_t pending = __ballot(mine >= 0), have = 0;
-    int i = 0, j = wave;
+    int i = 0, j = wave, before = 0;                       // before: blocks of the adapters before this one
     const auto adapter = [&] {
         i = __builtin_amdgcn_readlane(mine, __builtin_ctzll(pending));
         have = __ballot(mine == i);
+        start = mine == i ? before & (W - 1) : start;
     };
     const auto settle = [&] {                              // to the block j of adapter i, which may be a later one's
         while (pending && j >= a.rblocks) {
             j -= a.rblocks;
+            before += a.rblocks;
             pending &= ~have;
             if (pending) adapter();
         }
@@ -583,10 +586,12 @@ __device__ __forceinline__ void add_adapters(const LoraArgs &a, int mine, int ch
 #pragma unroll
         for (int n = 0; n < NB; ++n) hv[n] = load_h(a, min(row0 + n * 16 + rsel, a.rows - 1), j, quad);
     };
-    if (!pending) return;
+    start = 0;
+    if (!pending) return false;
     adapter();
     settle();
-    if (pending) load();
+    if (!pending) return false;
+    load();
     while (pending) {
         uint4v b[MB], h[NB];
 #pragma unroll
@@ -599,6 +604,16 @@ __device__ __forceinline__ void add_adapters(const LoraArgs &a, int mine, int ch
         if (pending) load();
         multiply_adapter<T>([&](int n) { return ((own >> (n * 16 + rsel)) & 1) != 0; }, b, [&](int n) { return h[n]; }, acc);
     }
+    return true;
+}
+
+// Block e of the waves' sums of an adapter, that of its first block (`start`) first: the order of a row's sum is its own, not that of
+// the adapters beside it.
+template <int W> __device__ __forceinline__ float4v get_adapter_sum(const unsigned char *lds, int part_bytes, int e, int lane, int start, int rblocks)
+{
+    float4v t = reinterpret_cast<const float4v *>(lds + start * part_bytes)[e * 64 + lane];
+    for (int q = 1; q < min(W, rblocks); ++q) t += reinterpret_cast<const float4v *>(lds + ((start + q) & (W - 1)) * part_bytes)[e * 64 + lane];
+    return t;
 }
 
 // The tail of a lane's four channels of a token.
@@ -644,6 +659,7 @@ template <typename T> __global__ __launch_bounds__(256) void lora_pack_kernel(Lo
 // reading is all of it (64 rows 4096 -> 4096: 3.0 us alone, 5.2 with adapters).  kAnyRows: rows at any element, operands straight from
 // memory, 30 GB/s a CU (1200 rows 2001 -> 2000 in bf16 155 us): left for tensors that begin between 16-byte pieces and for short rows.
 enum { kAnyRows = 0, kParts = 2 };
+constexpr size_t waves_lds(int mb, int nb, int w) { return (size_t)w * mb * nb * 1024 * (w * mb * nb <= 32 ? 2 : 1); }
 template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bounds__(64 * W, 2) void linear_lora_waves_kernel(LoraArgs a)
 {
     constexpr int kPart = MB * NB * 1024;
@@ -672,11 +688,35 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
                                                       static_cast<const T *>(a.w) + (size_t)ch0 * a.c, a.k - ch0, a.c, wave,
                                                       (a.c + 8 * kPer16<T> - 1) / (8 * kPer16<T>), part, lane, acc);
     }
-    if (a.adapters > 0) add_adapters<T, MB, NB, W>(a, mine, ch0, row0, lane, wave, acc);
+    // The adapters' sums lie apart from the product's, beside them where 64 KB hold both, else in their place later: which wave has
+    // them depends on the adapters of the other rows.
+    constexpr size_t kMore = waves_lds(MB, NB, W) / 2;
+    constexpr bool kBeside = kMore == (size_t)W * kPart;
+    float4v more[MB][NB];
+    clear(more);
+    int start = 0;
+    const bool any = a.adapters > 0 && add_adapters<T, MB, NB, W>(a, mine, ch0, row0, lane, wave, start, more);
     put_sums(part, lane, acc);
+    if (kBeside && any) put_sums(part + kMore, lane, more);
     __syncthreads();
-    for (int e = wave; e < MB * NB; e += W)
-        store4<T>(a, row0 + e % NB * 16 + rsel, ch0 + e / NB * 16 + quad * 4, get_sum<W>(lds, kPart, e, lane));
+    constexpr int kMine = (MB * NB + W - 1) / W;           // blocks of 16 x 16 that a wave stores
+    float4v t[kMine];
+#pragma unroll
+    for (int u = 0; u < kMine; ++u)
+        if (wave + u * W < MB * NB) t[u] = get_sum<W>(lds, kPart, wave + u * W, lane);
+    if (!kBeside && a.adapters > 0) {
+        __syncthreads();
+        if (any) put_sums(part, lane, more);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+        const int e = wave + u * W, token = e % NB * 16 + rsel;
+        if (e >= MB * NB) break;
+        const int adapter = __shfl(mine, token), first = __shfl(start, token);
+        if (adapter >= 0) t[u] += get_adapter_sum<W>(lds + (kBeside ? kMore : 0), kPart, e, lane, first, a.rblocks);
+        store4<T>(a, row0 + token, ch0 + e / NB * 16 + quad * 4, t[u]);
+    }
 }
 
 // Few rows: the first workgroups make h, the others parts of the product, 16 NB tokens x 16 MB channels over a part of the
@@ -722,7 +762,7 @@ template <typename K> bool allow_lds(K kernel, size_t bytes)
 template <typename T, int MB, int NB, int W, int MODE> tvg_status launch_waves(LoraArgs a, hipStream_t stream)
 {
     const auto kernel = linear_lora_waves_kernel<T, MB, NB, W, MODE>;
-    constexpr size_t kLds = (size_t)W * MB * NB * 1024;
+    constexpr size_t kLds = waves_lds(MB, NB, W);
     static const bool ok = allow_lds(kernel, kLds);
     if (!ok) return TVG_ERR_LAUNCH;
     a.tiles_n = (a.k + 16 * MB - 1) / (16 * MB);
