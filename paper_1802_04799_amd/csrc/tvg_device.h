@@ -117,17 +117,24 @@ __device__ __forceinline__ float relu_floor(bool relu)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(relu ? 0u : 0x7FC00000u));
 }
 
-// 1 / (1 + exp(-z)).  PRECISE: from e = exp(-|z|), 1 / (1 + e) and, below zero, e / (1 + e), which reach 1 and 0 at the ends; e is 2^n
-// exp2(f) with n + f = -|z| log2(e), f to 2^-24 from log2(e) in two parts, and zero beyond 104.  Values that are rounded to bf16 do
-// without: half a step of the product, |z| 2^-24 of the result, and zero where the result would be below 2^-126.
-template <bool PRECISE> __device__ __forceinline__ float sigmoid(float z)
+// s = 1 / (1 + exp(-z)) and rest = 1 - s: from e = exp(-|z|), 1 / (1 + e) and e / (1 + e), which reach 1 and 0 at the ends and lose no
+// digits in between.  e is 2^n exp2(f) with n + f = -|z| log2(e), f to 2^-24 from log2(e) in two parts, and zero beyond 104.
+struct Sigmoid { float s, rest; };
+__device__ __forceinline__ Sigmoid sigmoid_and_rest(float z)
 {
-    if constexpr (!PRECISE) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269502f * z));
     const float a = fminf(fabsf(z), 104.0f);               // (104 of a NaN, which stays one in what multiplies z)
     const float n = rintf(-1.44269502f * a);
     const float f = fmaf(-1.92596299e-8f, a, fmaf(-1.44269502f, a, -n));
-    const float e = ldexpf(__builtin_amdgcn_exp2f(f), (int)n), r = __builtin_amdgcn_rcpf(1.0f + e);
-    return z < 0.0f ? e * r : r;
+    const float e = ldexpf(__builtin_amdgcn_exp2f(f), (int)n), r = __builtin_amdgcn_rcpf(1.0f + e), t = e * r;
+    return z < 0.0f ? Sigmoid{t, r} : Sigmoid{r, t};
+}
+
+// s alone.  Values that are rounded to bf16 (not PRECISE) do with half a step of the product, |z| 2^-24 of the result, and zero
+// where the result would be below 2^-126.
+template <bool PRECISE> __device__ __forceinline__ float sigmoid(float z)
+{
+    if constexpr (PRECISE) return sigmoid_and_rest(z).s;
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269502f * z));
 }
 
 template <typename T> struct Elem;

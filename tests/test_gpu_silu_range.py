@@ -73,3 +73,32 @@ def test_silu_of_a_projection(tvg, rows, k, dtype):
         y = tvg.linear_lora_fused(x, w, None, None, None, activation="silu", **kw)
         same_or_within(y[rows - 1], want, bound)
         assert torch.equal(y.nan_to_num(7), y[rows - 1].nan_to_num(7).expand(rows, k))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pixels", [49, 40000])
+def test_derivative_of_silu(tvg, pixels, dtype):
+    """One pixel with a gradient, mean 0 and rstd 1: dbeta is act'(x) there, s + z s (1 - s), whose two terms have 10 roundings
+    each (s 7, z and 1 - s one each, the sum).  dgamma is x times that.  The bf16 form: exp(-z) has an error of |z| half steps of
+    its own beside that, which is |z| s below zero; above, 1 - s is a difference with |z| (1 - s) + 6 half steps of 1, times z, and zero
+    from z = 18 on, where 1 + exp(-z) is 1."""
+    import torch
+    to = torch.bfloat16 if dtype == "bf16" else torch.float32
+    z = far(dtype)
+    z = torch.where(torch.isfinite(z), z, torch.zeros_like(z))
+    x, dy = torch.zeros((1, pixels, 96), dtype=to, device="cuda"), torch.zeros((1, pixels, 96), dtype=to, device="cuda")
+    x[0, pixels // 3] = z.to(to)
+    dy[0, pixels // 3] = 1
+    mean, rstd = torch.zeros((1, 96), device="cuda"), torch.ones((1, 96), device="cuda")
+    one, zero = torch.ones(96, device="cuda"), torch.zeros(96, device="cuda")
+    _, dgamma, dbeta = tvg.group_norm_fused_backward(x, dy, mean, rstd, 96, one, zero, activation="silu")
+    v = z.double()
+    e = torch.exp(-v.abs())
+    s, rest = torch.where(v >= 0, 1 / (1 + e), e / (1 + e)), torch.where(v >= 0, e / (1 + e), 1 / (1 + e))
+    want = s + v * s * rest
+    bound = 10 * H * (s + (v * s * rest).abs()) + (v.abs() + 1) * 2.0 ** -149
+    if dtype == "bf16":
+        bound += H * torch.where(v > 0, v.clamp(max=18) * (v.clamp(max=18) * rest + 6), v.abs() * s * (1 + v.abs())) + (v.abs() + 1) * 2.0 ** -125 * (v < 0)
+    same_or_within(dbeta, want, bound)
+    small = v.abs() < 1e18
+    same_or_within(dgamma[small], (want * v)[small], (bound * v.abs() + H * (want * v).abs() + 2.0 ** -149)[small])
