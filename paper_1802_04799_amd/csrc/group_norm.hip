@@ -205,7 +205,7 @@ __device__ __forceinline__ void join_rows(const typename Vec<T, V>::type (&raw)[
     for (int i = 0; i < V; ++i) {
         const float d = sum[i] - mean[i];
         mean[i] = fmaf(d, share, mean[i]);
-        m2[i] += fmaf(d * d, cross, sq[i]);
+        m2[i] += fmaf(d, d * cross, sq[i]);                // (of the first rows cross is 0, d the mean, whose square may be infinite)
     }
 }
 
@@ -297,7 +297,7 @@ template <typename T, int V, bool WHOLE> __global__ __launch_bounds__(kThreads) 
                 const float before = o[0], all = before + total, d = m - o[1];
                 o[0] = all;
                 o[1] += d * (total / all);
-                o[2] += q + d * d * (before * (total / all));
+                o[2] += q + d * (d * (before * (total / all)));        // (as above)
             }
         }
     }
