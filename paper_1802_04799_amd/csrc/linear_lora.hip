@@ -322,7 +322,10 @@ template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __for
         for (int e = wave; e < NB * JB; e += W) {
             const int row = row0 + e % NB * 16 + rsel, j = j0 + e / NB;
             if (j >= a.rblocks || adapter_of(a, row) != i) continue;
-            const float4v h = get_sum<W>(lds, kPart, e, lane) * scale;
+            float4v h = get_sum<W>(lds, kPart, e, lane) * scale;
+            // (beyond the rank A's rows are zeros, which an infinity of x or of the scale makes a NaN)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) h[v] = j * 16 + quad * 4 + v < a.rank ? h[v] : 0.0f;
             unsigned char *to = a.h + ((size_t)row * a.rblocks + j) * 64;
             if constexpr (sizeof(T) == 4) *reinterpret_cast<float4v *>(to + quad * 16) = h;
             else {
