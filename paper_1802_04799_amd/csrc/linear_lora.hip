@@ -287,6 +287,8 @@ template <int N> __device__ __forceinline__ int distinct_adapters(const int (&mi
     return found;
 }
 
+constexpr float kLargestBf16 = 0x1.FEp127f;
+
 // h of NB blocks of 16 tokens and JB blocks of 16 ranks; the waves take 128 bytes of the reduction in turn and add up through
 // LDS.  Adapters of the tile: every slots-th of them.  Bound by reading x, once per adapter of the tile: 8192 rows of 4096 (67 MB)
 // with 16 adapters of rank 32 25 us, 2.7 TB/s.  h leaves in bf16 as two numbers, whose sum has an error of 2^-17.
@@ -332,8 +334,10 @@ template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __for
                 float f[4], lo[4];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    f[v] = h[v];
-                    const float d = h[v] - bf16_to_f32(f32_to_bf16(h[v]));
+                    // (a finite number stays one: what bf16 would round to infinity has its largest number as upper part)
+                    f[v] = __builtin_amdgcn_fmed3f(h[v], -kLargestBf16, kLargestBf16);
+                    f[v] = fabsf(h[v]) < INFINITY ? f[v] : h[v];
+                    const float d = h[v] - bf16_to_f32(f32_to_bf16(f[v]));
                     lo[v] = d == d ? d : 0.0f;             // (of an infinity the upper part is all)
                 }
                 *reinterpret_cast<uint2v *>(to + quad * 8) = Group4<bf16_t>::pack(f);

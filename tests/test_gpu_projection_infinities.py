@@ -35,3 +35,20 @@ def test_an_infinity_in_a_row(tvg, rows, k, shifted, rank, dtype):
     y = tvg.linear_lora_fused(x, w, a, b, index, scale)
     keep = index != index[at]
     assert bool((y[~keep] == INF).all()) and torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.parametrize("rows,k", [(1, 64), (60, 260), (1100, 1100)])
+def test_a_middle_vector_between_the_largest_numbers_of_bf16_and_of_fp32(tvg, rows, k):
+    """h = 1.003 times bf16's largest number, which fp32 holds and bf16 rounds to infinity; y = h / 2^20.  The sum of both parts is
+    within 2^-17 of h, y rounds once."""
+    import torch
+    x = torch.zeros((rows, 64), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((k, 64), dtype=torch.bfloat16, device="cuda")
+    x[:, 5] = torch.finfo(torch.bfloat16).max
+    a, b = torch.zeros((2, 16, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, k, 16), dtype=torch.bfloat16, device="cuda")
+    a[1, 3, 5], b[1, :, 3] = 1, 2.0 ** -20
+    for sign in (1.0, -1.0):
+        scale = torch.tensor([1.0, sign * 1.003], device="cuda")
+        y = tvg.linear_lora_fused(x, w, a, b, torch.ones(rows, dtype=torch.int32, device="cuda"), scale)
+        want = float(scale[1]) * torch.finfo(torch.bfloat16).max * 2.0 ** -20
+        assert bool(((y.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -17 + 4 * H) * abs(want)).all())
