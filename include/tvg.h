@@ -317,8 +317,9 @@ tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const 
  *   bias     device, fp32 [k], or NULL         residual  device, [rows][k], dtype, or NULL
  *   y        device, [rows][k], dtype, written completely; may be residual, else must not overlap an input
  * All sums are fp32, the adapter's middle vector too: bf16 operands of the matrix cores hold it in two parts, 16 bits together.
- * A row's result does not depend on the adapters of the other rows (what they hold, infinities and NaN included), and sums are
- * added in a fixed order.
+ * A row's result does not depend on the adapters of the other rows (which they are, and what they hold, infinities and NaN
+ * included), and sums are added in a fixed order.  Infinities come out as the formula has them, but for one in b with bf16: the two
+ * parts may make a NaN of it.
  * rows == 0 is TVG_OK and launches nothing.  adapters == 0 is a plain projection: a, b, adapter and scale are ignored.
  * flags must be 0.  Any alignment of whole elements; the fast way is 16-byte alignment of x, w, a and y, c and k multiples of 8
  * (bf16) or 4 (fp32).  For other c the workspace may hold copies of x, w and a with longer rows, made by every call.

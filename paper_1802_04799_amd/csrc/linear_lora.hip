@@ -17,8 +17,9 @@
 // vector costs no digits.
 //
 // Rows of a tile with different adapters: a pass per adapter in use, whose sums the tokens that have the adapter take and the
-// others do not; blocks of 16 tokens without it are skipped.  Nothing is multiplied by zero, so what an adapter holds
-// (infinities, NaN) reaches no other row, and a row's bits do not depend on the rows beside it.
+// others do not; blocks of 16 tokens without it are skipped.  No row is multiplied with another's adapter, not by zero either, so
+// what an adapter holds (infinities, NaN) reaches no other row, and a row's bits do not depend on the rows beside it.  Of its own
+// adapter an infinity in B meets both parts of h in bf16, of which one may be zero or of the other sign: a NaN then.
 #include <algorithm>
 #include <type_traits>
 #include <utility>

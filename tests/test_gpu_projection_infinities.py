@@ -52,3 +52,28 @@ def test_a_middle_vector_between_the_largest_numbers_of_bf16_and_of_fp32(tvg, ro
         y = tvg.linear_lora_fused(x, w, a, b, torch.ones(rows, dtype=torch.int32, device="cuda"), scale)
         want = float(scale[1]) * torch.finfo(torch.bfloat16).max * 2.0 ** -20
         assert bool(((y.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -17 + 4 * H) * abs(want)).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k,shifted", [(1, 64, False), (20, 64, False), (60, 260, False), (1100, 1100, False), (2100, 2060, False),
+                                            (4100, 2600, False), (1100, 1100, True)])
+def test_an_infinity_in_b(tvg, rows, k, shifted, dtype):
+    """One channel of one adapter: infinite in its rows in fp32, infinite or not a number in bf16, and nothing else changes."""
+    import torch
+    to = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    u = lambda *s: (torch.rand(s, generator=g, device="cuda") + 0.5).to(to)
+    x, w, a, b = u(rows, 128), u(k, 128), u(3, 12, 128), u(3, k, 12)
+    if shifted:
+        room = torch.zeros(b.numel() + 8, dtype=to, device="cuda")
+        b = room[1:1 + b.numel()].view(b.shape).copy_(b)
+        room = torch.zeros(x.numel() + 8, dtype=to, device="cuda")
+        x = room[1:1 + x.numel()].view(x.shape).copy_(x)
+    index = torch.randint(0, 3, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    clean = tvg.linear_lora_fused(x, w, a, b, index)
+    b[int(index[0]), k // 2, 7] = INF
+    y = tvg.linear_lora_fused(x, w, a, b, index)
+    hit = torch.zeros(y.shape, dtype=torch.bool, device="cuda")
+    hit[index == index[0], k // 2] = True
+    assert bool((y[hit] == INF).all()) if dtype == "f32" else not bool(torch.isfinite(y[hit]).any())
+    assert torch.equal(y[~hit], clean[~hit])
