@@ -438,7 +438,9 @@ template <typename T, int NB, int JB, bool WIDE> __global__ __launch_bounds__(64
         order_rows<64 * kShrinkWaves>(a, lds);
         return;
     }
-    shrink_tile<T, NB, JB, kShrinkWaves, WIDE, kHalfLds>(a, blockIdx.x - (a.order ? 1 : 0), lds);
+    const uint32_t b = blockIdx.y * gridDim.x + blockIdx.x - (a.order ? 1 : 0);
+    if (b >= (uint32_t)a.shrink_groups) return;
+    shrink_tile<T, NB, JB, kShrinkWaves, WIDE, kHalfLds>(a, b, lds);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1110,7 +1112,10 @@ template <typename T, int NB, int JB, bool WIDE> tvg_status launch_shrink(LoraAr
     const int tiles = (a.rows + 16 * NB - 1) / (16 * NB) * ((a.rblocks + JB - 1) / JB);
     // few tiles: their adapters in turn by several workgroups
     a.slots = std::max(1, std::min(std::min(16 * NB, std::min(a.rows, a.adapters)), 2 * kComputeUnits / tiles));
-    hipLaunchKernelGGL(kernel, dim3(tiles * a.slots + (a.order ? 1 : 0)), dim3(64 * W), kLds, stream, a);
+    a.shrink_groups = tiles * a.slots;
+    // (a launch has fewer than 2^32 work items in x: 8.4 million rows of rank 256 would pass that, and lose the rows behind)
+    const int in_x = std::min(a.shrink_groups, 1 << 22), in_y = (a.shrink_groups + in_x - 1) / in_x;
+    hipLaunchKernelGGL(kernel, dim3(in_x + (a.order ? 1 : 0), in_y), dim3(64 * W), kLds, stream, a);
     return hipGetLastError() == hipSuccess ? TVG_OK : TVG_ERR_LAUNCH;
 }
 
