@@ -39,3 +39,16 @@ def test_many_rows(tvg, rows, c, k, rank):
     at = torch.cat([torch.arange(300, device="cuda"), torch.arange(rows - 300, rows, device="cuda"),
                     torch.randint(0, rows, (3000,), generator=g, device="cuda")])
     check_some(y, x, w, a, b, index, at)
+
+
+@pytest.mark.parametrize("rows,c,k", [(3, (1 << 22) + 8, 5), (3, (1 << 23) + 3, 5), (40, (1 << 22) + 8, 70)])
+def test_the_longest_rows(tvg, rows, c, k):
+    """Rows of 8 MB and more are read at any element."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(c)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)
+    x, w, a, b = r(rows, c), r(k, c) * c ** -0.5, r(3, 4, c) * c ** -0.5, r(3, k, 4)
+    index = torch.randint(-1, 4, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    y = tvg.linear_lora_fused(x, w, a, b, index)
+    torch.cuda.synchronize()
+    check_some(y, x, w, a, b, index, torch.arange(rows, device="cuda"))
