@@ -7,7 +7,8 @@
 //   with a, b the sums of gamma S1, gamma S2 over a group's channels and m its elements
 //
 // Bound by memory: about 10 (forward) or 25 (backward) operations an element.  Where a block of channels of a sample fits a
-// workgroup's registers one launch reads it once (32 maps 56x56x256 in bf16, 51 MB: 29 us, 3.6 TB/s of a copy's 5.1).  Else two
+// workgroup's registers one launch reads it once (32 maps 56x56x256 in bf16, 51 MB read and written: 25 us a call among others, 4.1 TB/s
+// of a copy's 5.1; 29 us in a trace, whose calls have gaps and colder caches, as the times of single kernels below).  Else two
 // launches: the first leaves partial statistics of row chunks in the workspace, the second joins those of its sample in a fixed
 // order and applies them, the last chunk first: it is the one whose rows the caches still hold (64 maps 112x112x256, 411 MB: 74 us
 // and 149, 5.5 TB/s over both reads and the write; backward 147 us and 219, 5.6 TB/s over four reads and a write).
@@ -112,7 +113,7 @@ struct NormArgs {
     int tiles;                             // n * blocks * chunks
     float eps;
     int act;
-    int passing;                           // results pass the caches by, and so does x when it is read last
+    int passing;                           // one launch: results pass the caches by; two: x does when it is read last (results always do)
 };
 
 // The part of the problem that a workgroup has.
@@ -1104,7 +1105,7 @@ static void plan_group_norm(const NormProblem &p, int vector, bool backward, Nor
 }
 
 // The workspace holds what any alignment of the tensors needs.
-static size_t largest_workspace(const NormProblem &p, bool backward)
+size_t group_norm_workspace(const NormProblem &p, bool backward)
 {
     size_t bytes = 0;
     NormPlan plan;
@@ -1113,11 +1114,6 @@ static size_t largest_workspace(const NormProblem &p, bool backward)
         bytes = std::max(bytes, (plan.part_floats + (backward ? plan.chan_floats : 0)) * sizeof(float));
     }
     return bytes;
-}
-
-size_t group_norm_workspace(const NormProblem &p, bool backward)
-{
-    return largest_workspace(p, backward);
 }
 
 tvg_status launch_group_norm(const NormProblem &p, const void *x, const float *gamma, const float *beta, void *y, float *mean,

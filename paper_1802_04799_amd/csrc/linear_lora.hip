@@ -4,8 +4,8 @@
 // Two launches.  The first makes the adapters' middle vectors h = scale_i A_i x.  The second is a matrix product whose
 // reduction goes on, after the c channels, over the rank: the same accumulators take B_i h.  With few tiles the first launch makes
 // h and the product in parts of the reduction, the second adds both up.  Many rows are bound by the matrix cores and what feeds
-// them (8192 rows 4096 -> 4096 in bf16: 25 us for h, 207 for the product, 1.33 PFLOP/s), few by the weights' bytes and the two
-// launches (64 rows 4096 -> 4096: 10.9 and 3.0 us for 34 MB).
+// them (8192 rows 4096 -> 4096 in bf16: 222 us without adapters, 1.24 PFLOP/s, 251 with 16 of rank 32), few by the weights' bytes and
+// the two launches (64 rows 4096 -> 4096: 14.9 us without adapters, 19.8 with 32 of rank 16).
 //
 // Both types are the same kernels in bytes: a lane's operand of a 16x16 tile is 16 bytes, 8 bf16 of one
 // v_mfma_f32_16x16x32_bf16 or 4 fp32 of four v_mfma_f32_16x16x4_f32, whose order of the reduction is that of the loads.
@@ -292,7 +292,7 @@ constexpr float kLargestBf16 = 0x1.FEp127f;
 
 // h of NB blocks of 16 tokens and JB blocks of 16 ranks; the waves take 128 bytes of the reduction in turn and add up through
 // LDS.  Adapters of the tile: every slots-th of them.  Bound by reading x, once per adapter of the tile: 8192 rows of 4096 (67 MB)
-// with 16 adapters of rank 32 25 us, 2.7 TB/s.  h leaves in bf16 as two numbers, whose sum has an error of 2^-17.
+// with 16 adapters of rank 32, eight requests, 28 us, 2.4 TB/s.  h leaves in bf16 as two numbers, whose sum has an error of 2^-17.
 template <typename T, int NB, int JB, int W, bool WIDE, int KB> __device__ __forceinline__ void shrink_tile(const LoraArgs &a, int b, unsigned char *lds)
 {
     constexpr int kPart = kPartBytes<T, JB, NB, W, WIDE, KB>;
@@ -666,7 +666,7 @@ template <typename T> __global__ __launch_bounds__(256) void lora_pack_kernel(Lo
 
 // A workgroup has 16 NB tokens x 16 MB channels and its waves split the reduction, without a barrier; then they take the
 // adapters' blocks of ranks in turn, and add up through LDS.  kParts: the product is there already, in parts of the reduction, whose
-// reading is all of it (64 rows 4096 -> 4096: 3.0 us alone, 5.2 with adapters).  kAnyRows: rows at any element, operands straight from
+// reading is all of it (64 rows 4096 -> 4096, traced: 4.0 us without adapters, 6.8 with 32).  kAnyRows: rows at any element, operands straight from
 // memory, 30 GB/s a CU (1200 rows 2001 -> 2000 in bf16 155 us): left for tensors that begin between 16-byte pieces and for short rows.
 enum { kAnyRows = 0, kParts = 2 };
 constexpr size_t waves_lds(int mb, int nb, int w) { return (size_t)w * mb * nb * 1024 * (w * mb * nb <= 32 ? 2 : 1); }
@@ -730,8 +730,8 @@ template <typename T, int MB, int NB, int W, int MODE> __global__ __launch_bound
 }
 
 // Few rows: the first workgroups make h, the others parts of the product, 16 NB tokens x 16 MB channels over a part of the
-// reduction, which the next launch adds up.  64 rows 4096 -> 4096 in bf16: 10.9 us for the weights' 34 MB (3.1 TB/s; 12.7 with h of 32
-// adapters), where the library's product takes 19; one row 1024 -> 1024 4.2 us, a launch's latency.
+// reduction, which the next launch adds up.  64 rows 4096 -> 4096 in bf16, traced: 12.1 us for the weights' 34 MB (2.8 TB/s; 13.3 beside
+// h of 32 adapters); one row 1024 -> 1024 4.2 us, a launch's latency.
 template <typename T, int MB, int NB, bool WIDE> __global__ __launch_bounds__(64 * product_waves(MB, NB), 2) void lora_parts_kernel(LoraArgs a)
 {
     constexpr int W = product_waves(MB, NB), kPart = kPartBytes<T, MB, NB, W, WIDE, kAllLds>;
@@ -1190,7 +1190,9 @@ int ring_tile(const LoraProblem &p)
 // 1997 and 3260), 1200 rows 2001 -> 2000 49 and 171 (132 and 181), 1200 rows 133 -> 2000 19 and 24 (33 and 34), 1000 rows
 // 131 -> 1040, the smallest copied, 17 and 15 (24 and 20).  With fewer tiles where that is as much work as 16 rows 4096 -> 4096, and
 // in bf16: 16 rows 4097 -> 4096 28 and 34, 64 rows 29 and 82, 777 rows 1001 -> 515 18 and 28, 64 rows 1001 -> 1024 13 and 12; fp32, whose
-// products take longer, 100 rows 4097 -> 4096 98 and 77, 777 rows 1001 -> 515 36 and 32.  Not where the adapters, of which a call
+// products take longer, 100 rows 4097 -> 4096 98 and 77, 777 rows 1001 -> 515 36 and 32.  Rows of 1000 to 2000 elements cross there: 64 rows
+// 1001 -> 1024 13.9 and 12.4, 2001 -> 2048 21.5 and 19.9, 200 rows 17.4 and 20.8, 25 and 57; longer ones do further down, which this leaves (16
+// rows 4097 -> 1024 22 and 35, 1 row 18 and 23).  Not where the adapters, of which a call
 // may use a few, would be most of the copy.
 size_t elem_size(const LoraProblem &p) { return p.dtype == TVG_BF16 ? 2 : 4; }
 int packed_c(const LoraProblem &p)
