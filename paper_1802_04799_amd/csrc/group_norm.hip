@@ -618,7 +618,7 @@ __global__ __launch_bounds__(kThreads) void group_norm_grad_apply_kernel(NormArg
         float sa[V], sb[V];
         for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
             sa[i] = ga[g] * k.rstd[i];
-            sb[i] = gb[g] * (k.rstd[i] * k.rstd[i]);
+            sb[i] = gb[g] * k.rstd[i] * k.rstd[i];             // (rstd^2 alone may be infinite)
         });
         for (; row < t.row1; row += U * t.rp, load()) {
 #pragma unroll
@@ -902,7 +902,7 @@ template <typename T, int V, int NV, int THREADS, bool WHOLE> __global__ __launc
     float sa[V], sb[V];
     for_channels<V, WHOLE>(cc, a.cpg, [&](int i, int g) {
         sa[i] = group[2 * g] * k.rstd[i];
-        sb[i] = group[2 * g + 1] * (k.rstd[i] * k.rstd[i]);
+        sb[i] = group[2 * g + 1] * k.rstd[i] * k.rstd[i];  // (rstd^2 alone may be infinite)
     });
     const auto write = [&](auto act, auto pass) {
         rows(act, [&](int u, float (&fx)[V], auto &&dz_of) {

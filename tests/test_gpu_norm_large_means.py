@@ -31,3 +31,24 @@ def test_a_mean_whose_square_is_beyond_fp32(tvg, shape, groups, dtype):
     assert bool((var >= low * (1 - 4 * H)).all()) and bool((var <= high * (1 + 4 * H)).all())
     want = (v - mean.double().view(shape[0], 1, groups, 1)) * rstd.double().view(shape[0], 1, groups, 1)
     assert bool(((y.double().view(v.shape) - want).abs() <= (4 * H + HALF[dtype]) * want.abs() + 1e-37).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pixels", [49, 40000])
+def test_gradients_of_constant_groups_whose_rstd_has_an_infinite_square(tvg, pixels, dtype):
+    """x is the mean everywhere and rstd 1e20, as of eps 1e-40: dx is rstd (gamma dz - a), a group's mean of gamma dz, in fewer than 200 roundings of
+    the terms (dy is +-1, +-2 or +-3, whose sums are exact; gamma rounds the rest)."""
+    import torch
+    to = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(pixels)
+    x = torch.full((2, pixels, 64), 1.5, dtype=to, device="cuda")
+    dy = torch.randint(1, 4, x.shape, generator=g, device="cuda") * (torch.randint(0, 2, x.shape, generator=g, device="cuda") * 2 - 1)
+    dy, gamma, beta = dy.to(to), torch.rand(64, generator=g, device="cuda") + 0.5, torch.zeros(64, device="cuda")
+    mean, rstd = torch.full((2, 8), 1.5, device="cuda"), torch.full((2, 8), 1e20, device="cuda")
+    dx, dgamma, dbeta = tvg.group_norm_fused_backward(x, dy, mean, rstd, 8, gamma, beta)
+    dz = (dy.double() * gamma.double()).view(2, pixels, 8, 8)
+    a, r = dz.mean(dim=(1, 3), keepdim=True), rstd.double().view(2, 1, 8, 1)
+    size = r * (dz.abs() + dz.abs().mean(dim=(1, 3), keepdim=True))
+    want = r * (dz - a)
+    assert bool(((dx.double().view(want.shape) - want).abs() <= 200 * H * size + HALF[dtype] * want.abs()).all())
+    assert bool((dgamma == 0).all()) and torch.equal(dbeta.double(), dy.double().sum((0, 1)))
