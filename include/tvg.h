@@ -315,7 +315,7 @@ tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const 
  *   adapter  device, int32 [rows]; any value outside [0, adapters) is a row without an adapter
  *   scale    device, fp32 [adapters], or NULL (ones)
  *   bias     device, fp32 [k], or NULL         residual  device, [rows][k], dtype, or NULL
- *   y        device, [rows][k], dtype, written completely; may be residual, else must not overlap an input
+ *   y        device, [rows][k], dtype, written completely; may be residual (one that is not x), else must not overlap an input
  * All sums are fp32, the adapter's middle vector too: bf16 operands of the matrix cores hold it in two parts, 16 bits together.
  * A row's result does not depend on the adapters of the other rows (which they are, and what they hold, infinities and NaN
  * included), and sums are added in a fixed order.  Infinities come out as the formula has them, but for one in b with bf16: the two
@@ -324,7 +324,8 @@ tvg_status tvg_group_norm_fused_backward(const tvg_group_norm_desc *desc, const 
  * flags must be 0.  Any alignment of whole elements; the fast way is 16-byte alignment of x, w, a and y, c and k multiples of 8
  * (bf16) or 4 (fp32).  For other c the workspace may hold copies of x, w and a with longer rows, made by every call.
  * Errors: TVG_ERR_BAD_SHAPE for c, k or rank below 1, rows or adapters below 0; TVG_ERR_UNSUPPORTED for unknown dtype,
- * activation or flags, rank above 256, rows, c or k of 2^24 or more and tensors of 2^31 elements or more; TVG_ERR_WORKSPACE as above.
+ * activation or flags, rank above 256, rows, c or k of 2^24 or more, tensors of 2^31 elements or more and y over x; TVG_ERR_WORKSPACE
+ * as above.
  */
 typedef struct {
     int32_t rows, c, k, adapters, rank;

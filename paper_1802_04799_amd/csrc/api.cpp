@@ -759,6 +759,12 @@ static bool aligned_to(size_t bytes, std::initializer_list<const void *> pointer
     return true;
 }
 
+static bool overlap(const void *p, int64_t p_bytes, const void *q, int64_t q_bytes)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return p && q && a < b + (uintptr_t)q_bytes && b < a + (uintptr_t)p_bytes;
+}
+
 static tvg_status make_norm(const tvg_group_norm_desc *d, tvg::NormProblem *p)
 {
     if (!d) return TVG_ERR_NULL;
@@ -854,6 +860,9 @@ tvg_status tvg_linear_lora_fused(const tvg_linear_lora_desc *desc, const void *x
     if (!aligned_to(p.dtype == TVG_BF16 ? 2 : 4, {x, w, a, b, residual, y}) || !aligned_to(4, {adapter, scale, bias}))
         return TVG_ERR_UNSUPPORTED;
     if (!workspace_ok(workspace, workspace_bytes, tvg::linear_lora_workspace(p))) return TVG_ERR_WORKSPACE;
+    // (rows of x are read while others' sums are written: y over a residual that is x would take some of them for x)
+    const int64_t size = p.dtype == TVG_BF16 ? 2 : 4;
+    if (overlap(y, size * p.rows * p.k, x, size * p.rows * p.c)) return TVG_ERR_UNSUPPORTED;
     const tvg::LoraPointers ptr{x, w, a, b, adapter, scale, bias, residual, y, static_cast<float *>(workspace)};
     return tvg::launch_linear_lora(p, ptr, static_cast<hipStream_t>(hip_stream));
 }
